@@ -10,7 +10,7 @@ definitions in float64, and ``draw`` gives further cases of the same ranges.
 The cache of one layer is a triple:
   blocks [B, H_kv, blocks, 8192], one byte each: 32 tokens of K, then of V.
          K byte [kt][h][g][c][b] is token 16 kt + c, dim 64 h + 16 g + b;
-         V byte [u][g][c][t][j][i] is token 16 j + 4 g + i, dim 32 u + 16 t + c.
+         V byte [u][g][c][t][j][i] is token 16 j + 4 g + i, dim 8 c + 2 u + t.
          float8_e4m3fn values, or uint8 holding integers of -127..127 plus 128.
   scales [B, H_kv, blocks, 2] float32: what the K and V values are times.
   tail   [B, H_kv, 2, 128, 128] bfloat16: K and V rows of the tokens behind
@@ -368,9 +368,9 @@ def _pack_k(codes):
 
 def _pack_v(codes):
     lead = codes.shape[:-2]
-    x = codes.reshape(*lead, 2, 4, 4, 4, 2, 16)  # j g i u t c
+    x = codes.reshape(*lead, 2, 4, 4, 16, 4, 2)  # j g i c u t
     n = len(lead)
-    return x.permute(*range(n), n + 3, n + 1, n + 5, n + 4, n, n + 2).reshape(*lead, BLOCK * D)
+    return x.permute(*range(n), n + 4, n + 1, n + 3, n + 5, n, n + 2).reshape(*lead, BLOCK * D)
 
 
 def _unpack(blocks, scales, dtype):
@@ -380,7 +380,7 @@ def _unpack(blocks, scales, dtype):
     k = blocks[..., :BLOCK * D].reshape(*blocks.shape[:-1], 2, 2, 4, 16, 16)  # kt h g c b
     v = blocks[..., BLOCK * D:].reshape(*blocks.shape[:-1], 4, 4, 16, 2, 2, 4)  # u g c t j i
     k = k.permute(*range(n), n, n + 3, n + 1, n + 2, n + 4).reshape(*blocks.shape[:-1], BLOCK, D)
-    v = v.permute(*range(n), n + 4, n + 1, n + 5, n, n + 3, n + 2).reshape(*blocks.shape[:-1], BLOCK, D)
+    v = v.permute(*range(n), n + 4, n + 1, n + 5, n + 2, n, n + 3).reshape(*blocks.shape[:-1], BLOCK, D)
     off = 128 if blocks.dtype == torch.uint8 else 0
     k = (k.to(dtype) - off) * scales[..., 0, None, None].to(dtype)
     v = (v.to(dtype) - off) * scales[..., 1, None, None].to(dtype)
@@ -634,7 +634,7 @@ def _token_dims(part):
         kt, h, g, c, b = at // 2048, at // 1024 % 2, at // 256 % 4, at // 16 % 16, at % 16
         return 16 * kt + c, 64 * h + 16 * g + b
     u, g, c, t, j, i = at // 1024, at // 256 % 4, at // 16 % 16, at // 8 % 2, at // 4 % 2, at % 4
-    return 16 * j + 4 * g + i, 32 * u + 16 * t + c
+    return 16 * j + 4 * g + i, 8 * c + 2 * u + t
 
 
 def _exact_unpack(blocks, scales):
