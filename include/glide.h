@@ -29,6 +29,12 @@
  *                      and output projections (Sec. 4.1, Q^{m,j} and
  *                      MultiHead equations); glide_rows_matmul is its
  *                      few-row projection.
+ *   glide_rope         rotary positions of query and key rows, tree nodes at
+ *                      their depth behind the prefix; forward and backward.
+ *   glide_q8_append, glide_q8_read, glide_q8_commit, glide_q8_tree_attn
+ *                      a key/value cache held in 8 bits with a scale for each
+ *                      block of 32 tokens and head: rows written, read back
+ *                      and committed, and the tree / cross attention over it.
  *
  * Conventions shared by every call:
  *   - All array arguments are DEVICE pointers to memory the caller owns and
@@ -71,6 +77,10 @@ extern "C" {
 /* Element types of q / k_cache / v_cache / out. */
 #define GLIDE_BF16    0   /* bfloat16 in and out, float32 accumulation */
 #define GLIDE_F32     1   /* float32 in and out, float32 accumulation */
+
+/* How an 8-bit cache holds its blocks (glide_q8_cache). */
+#define GLIDE_E4M3    2   /* 8-bit floating point, 4 exponent and 3 mantissa bits */
+#define GLIDE_INT8    3   /* integers -127..127, each byte the value plus 128 */
 
 #define GLIDE_MAX_NODES   64   /* tree nodes / query rows per sequence */
 #define GLIDE_MAX_SPLITS  64   /* key-range splits per (sequence, head) */
@@ -399,6 +409,183 @@ int glide_block_attn(const void* q, const void* k_cache, const void* v_cache, vo
  * for arguments outside those ranges.  Host function, no GPU work.
  */
 double glide_expected_speedup(double alpha, int gamma, double c);
+
+/*
+ * ---------------------------------------------------------------------------
+ * Rotary positions, and a key/value cache held in 8 bits.
+ *
+ * The attention calls above take queries and keys with their positions already
+ * applied; glide_rope applies them.  A cache in 8 bits has half the bytes of a
+ * bfloat16 one, which is what the attention of a decoding step is bound by.
+ * ---------------------------------------------------------------------------
+ */
+
+/* Rows of glide_rope: row (b, t, h) of in starts at element
+ * b * in_strides[0] + t * in_strides[1] + h * in_strides[2] and holds D
+ * elements in a row; out likewise.  in == out with equal strides turns in
+ * place; otherwise they must not overlap.  Both 16-byte aligned, strides
+ * multiples of 8 (bfloat16) or 4 (float32). */
+typedef struct glide_rope_rows {
+  const void* in;
+  void* out;
+  int64_t in_strides[3], out_strides[3];
+  int H;
+} glide_rope_rows;
+
+#define GLIDE_ROPE_INTERLEAVED 1  /* pairs of dims (2i, 2i + 1), not (i, i + rot_dim / 2) */
+#define GLIDE_ROPE_BACKWARD    2  /* the transposed map: gradients of out to gradients of in */
+
+/*
+ * glide_rope -- rotary positions: pair i of the first rot_dim dims of a row at
+ * position p becomes
+ *   y1 = m (x1 cos a - x2 sin a),  y2 = m (x2 cos a + x1 sin a),
+ *   a = p * freqs[i];
+ * dims at and past rot_dim are copied.  The backward pass has the sine's sign
+ * changed.
+ *   q, k      HOST structs of B x T x H rows each; k may be NULL.
+ *   freqs     [rot_dim / 2] float64 (device), mscale (m) a factor of the
+ *             rotated dims: see glide_rope_frequencies.
+ *   position of row (b, t), from DEVICE int32 arrays, each nullable:
+ *             positions[b, t] if positions [B, T] is given (then the other two
+ *             must be NULL); else seq_lens[b] (0 without) plus t, or plus the
+ *             number of node t's ancestors if tree_parents [B, T] is given:
+ *             the positions of a tree behind a prefix of seq_lens[b] tokens.
+ *   D == 128; 2 <= rot_dim <= D, even; T >= 1 (tree: <= 64);
+ *   1 <= B <= 65535; H >= 1; B * T * (q->H + k->H) < 2^31;
+ *   dtype     GLIDE_BF16 or GLIDE_F32 (rows; arithmetic in float32, the angle
+ *             reduced in float64).
+ */
+int glide_rope(const glide_rope_rows* q, const glide_rope_rows* k, const double* freqs, int rot_dim,
+               float mscale, const int32_t* positions, const int32_t* seq_lens,
+               const int32_t* tree_parents, int B, int T, int D, int dtype, int flags,
+               hipStream_t stream);
+
+/* Scalings of glide_rope_frequencies for contexts longer than trained for. */
+#define GLIDE_ROPE_PLAIN  0  /* freqs[i] = base^(-2i / rot_dim) */
+#define GLIDE_ROPE_LINEAR 1  /* positions divided by factor */
+#define GLIDE_ROPE_NTK    2  /* base multiplied by factor^(rot_dim / (rot_dim - 2)) */
+#define GLIDE_ROPE_YARN   3  /* frequencies that turn less than once over original_len
+                                positions divided by factor, those that turn 32
+                                times or more kept, a linear ramp of the number of
+                                turns between; m = 0.1 ln(factor) + 1 */
+
+/*
+ * glide_rope_frequencies -- the frequencies and the factor m of a rotary
+ * embedding, into HOST memory: freqs [rot_dim / 2], mscale [1].
+ *   rot_dim even, 2..128 (4.. for GLIDE_ROPE_NTK); base > 1; factor >= 1;
+ *   original_len >= 1 for GLIDE_ROPE_YARN (not used otherwise).
+ * Host function, no GPU work.
+ */
+int glide_rope_frequencies(int rot_dim, double base, int scaling, double factor, int original_len,
+                           double* freqs, float* mscale);
+
+#define GLIDE_Q8_BLOCK       32    /* tokens of a block */
+#define GLIDE_Q8_BLOCK_BYTES 8192  /* K and V of a block and head */
+#define GLIDE_Q8_TAIL        128   /* rows of the ring */
+
+/*
+ * The cache of one layer in 8 bits (DEVICE pointers, 16-byte aligned), for
+ * L_cap tokens (a multiple of 32):
+ *   blocks  [B, H_kv, L_cap / 32, 8192] bytes: tokens 32 i .. 32 i + 31 in
+ *           block i.  Bytes 0..4095 K: byte ((kt * 2 + h) * 64 + 16 g + c) * 16
+ *           + e is token 16 kt + c, dim 64 h + 16 g + e (e < 16, c < 16, g < 4).
+ *           Bytes 4096..8191 V: byte (u * 64 + 16 g + c) * 16 + 8 t + 4 j + i is
+ *           token 16 j + 4 g + i, dim 8 c + 2 u + t (i, g, u < 4, j, t < 2).
+ *   scales  [B, H_kv, L_cap / 32, 2] float32: a K (V) value is its code times
+ *           the first (second).
+ *   tail    [B, H_kv, 2, 128, D] bfloat16: K and V rows of the tokens behind the
+ *           last whole block, and of the tree behind those; token j at row
+ *           j % 128.
+ * With a length L, tokens [0, 32 floor(L / 32)) are in blocks and the others in
+ * the tail.  A block is quantised once, when its last token is final: scale =
+ * max |x| / 448 (GLIDE_E4M3) or / 127 (GLIDE_INT8) over its 32 x 128 values,
+ * code = x / scale rounded to nearest even, both quotients float32; a scale
+ * below 2^-126 counts as 0, its block as zeros.  Values must be finite (an
+ * infinity or NaN makes its block's scale one).  Memory that holds no token of
+ * a sequence is never read as one, whatever it contains.
+ */
+typedef struct glide_q8_cache {
+  void* blocks;
+  float* scales;
+  void* tail;
+} glide_q8_cache;
+
+/*
+ * glide_q8_append -- writes T new rows of every sequence behind its length.
+ *   hold == 0: the rows are final (a prompt, decoded tokens).  Blocks that
+ *     become whole are quantised, from the tail and the new rows; the rows left
+ *     behind the last whole block go to the tail.  Rows past L_cap are dropped.
+ *     The caller's new lengths are seq_lens[b] + the rows written.
+ *   hold != 0: the rows are a tree's (T <= 64), to be verified: they go to the
+ *     tail alone, node t at row (seq_lens[b] + t) % 128, where
+ *     glide_q8_tree_attn reads and glide_q8_commit takes them.
+ *   k_new, v_new  [B, T, H_kv, D] bfloat16, row (b, t, h) at element
+ *     b * stride_b + t * stride_t + h * stride_h of each (strides non-negative
+ *     multiples of 8; 16-byte aligned).
+ *   seq_lens [B] int32, clamped to [0, L_cap]; counts [B] int32 or NULL: rows of
+ *     each sequence that are written (clamped to [0, T]; NULL: T).
+ *   D == 128; B, H_kv <= 65535; 1 <= T; 32 <= L_cap <= 4194304, a multiple of 32;
+ *   kind GLIDE_E4M3 or GLIDE_INT8.
+ */
+int glide_q8_append(const void* k_new, const void* v_new, int64_t stride_b, int64_t stride_t,
+                    int64_t stride_h, const int32_t* seq_lens, const int32_t* counts, int hold,
+                    const glide_q8_cache* cache, int B, int T, int H_kv, int D, int L_cap, int kind,
+                    hipStream_t stream);
+
+/*
+ * glide_q8_read -- tokens [start, start + T) of every sequence as bfloat16 or
+ * float32 rows, k_out and v_out [B, H_kv, T, D] of out_dtype (16-byte aligned):
+ * code * scale in float32, rounded to out_dtype once.  Rows at and past
+ * seq_lens[b] (clamped to [0, L_cap]) are left as they were.
+ *   0 <= start; 1 <= T; start + T <= L_cap + 31.
+ */
+int glide_q8_read(const glide_q8_cache* cache, const int32_t* seq_lens, void* k_out, void* v_out,
+                  int out_dtype, int B, int H_kv, int D, int L_cap, int kind, int start, int T,
+                  hipStream_t stream);
+
+/*
+ * glide_q8_tree_attn -- glide_tree_attn over an 8-bit cache: the query rows of
+ * sequence b see its tokens [0, seq_lens[b]) and, in tree mode, the tail rows of
+ * the nodes that are their own or an ancestor's (held by glide_q8_append).
+ *   q, out       [B, N, H, D] bfloat16, 16-byte aligned; H a multiple of H_kv:
+ *                query heads j * H / H_kv .. read cached head j.
+ *   seq_lens     [B] int32, clamped to [0, L_cap].
+ *   tree_parents [B, N] int32, or NULL (cross mode).
+ *   scale, max_splits, workspace: as glide_tree_attn (the workspace begins with
+ *                the same block of arrival counters, zero before its first use
+ *                and left zero by every call: one buffer can serve both).
+ *   1 <= N <= 64; B <= 65535; B * N * H < 2^31; D == 128.
+ * Precision: scores, sums and outputs accumulate in float32 from exact codes;
+ * probabilities enter the PV product with 11 significant bits (those below
+ * 2^-21 of a row's largest with fewer).  Tree rows that are not finite reach
+ * only the nodes that see them.
+ */
+size_t glide_q8_tree_attn_workspace(int B, int N, int H, int H_kv, int D, int L_cap, int max_splits);
+int glide_q8_tree_attn(const void* q, const glide_q8_cache* cache, const int32_t* seq_lens,
+                       const int32_t* tree_parents, void* out, int B, int N, int H, int H_kv, int D,
+                       int L_cap, int kind, float scale, int max_splits, void* workspace,
+                       size_t ws_bytes, hipStream_t stream);
+
+/*
+ * glide_q8_commit -- the accepted rows of a verification step become tokens of
+ * every layer's 8-bit cache: with L = seq_lens[b] clamped to [0, L_cap], token
+ * L + d takes the tail row of path node path[b, d], d < accept_len[b]; blocks
+ * that become whole are quantised; seq_lens_out[b] = L + accept_len[b] (rows
+ * past L_cap are dropped and not counted).
+ *   caches     HOST array of `layers` caches, 1 <= layers <= 128.
+ *   accept_len [B] int32 (clamped to [0, N]); path [B, N] int32 as
+ *              glide_verify_commit gives it (with layers == 0 there), or NULL:
+ *              the nodes are a chain, 0, 1, ... (spec_sample_verify).
+ *   seq_lens_out [B] int32 out (must not be seq_lens).
+ *   1 <= N <= 64; B, H_kv <= 65535; D == 128.  One launch.
+ */
+int glide_q8_commit(const glide_q8_cache* caches, int layers, const int32_t* seq_lens,
+                    const int32_t* accept_len, const int32_t* path, int32_t* seq_lens_out, int B,
+                    int N, int H_kv, int D, int L_cap, int kind, hipStream_t stream);
+
+/* Identifier of the graph capture that `stream` is under, 0 if it is under
+ * none: a workspace kept between eager calls must not serve a captured one. */
+unsigned long long glide_capture_id(hipStream_t stream);
 
 #ifdef __cplusplus
 }

@@ -28,6 +28,10 @@ This package is a plain, slow, obviously-correct restatement of what the paper
                     prefix in every layer's cache, the rest discarded, and the
                     new length (Sec. 3; Sec. 4.1, the cache kept after a
                     verification step).
+* ``rope``       -- rotary positions (not in the paper, whose target models
+                    apply them to the queries and keys of every layer).
+* ``q8``         -- a key/value cache held in 8 bits with a scale for each block
+                    of tokens and head (not in the paper), and attention over it.
 
 Only the test-suite, ``__graft_entry__.smoke()`` and the ``cpu_baseline`` leg
 of ``bench.py`` may import this package.  The HIP library never calls it and
@@ -40,4 +44,4 @@ causal-attention routine, the paper's own mask formula, closed forms, boundary
 tables and hand-derived golden fixtures).  No function is "parity unpinned".
 """
 
-from . import attention, block_attention, cape, commit, cross_block, spec_sampling, verify  # noqa: F401
+from . import attention, block_attention, cape, commit, cross_block, q8, rope, spec_sampling, verify  # noqa: F401

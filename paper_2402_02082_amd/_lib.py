@@ -6,7 +6,8 @@ name.  No computation happens in Python and there is no fallback: if the
 library is missing or a call fails, an exception is raised.
 
 glide_tree_attn, glide_verify_commit, cape_expand, spec_sample_verify,
-glide_rows_matmul and glide_block_attn try the native checks first (_native,
+glide_rows_matmul, glide_block_attn, glide_rope and the calls on an 8-bit
+cache (glide_q8_*) try the native checks first (_native,
 csrc/binding.cpp: the same checks and the same call); where those decline --
 an explicit stream, a tensor subclass, or anything that fails a check -- the
 Python checks below them decide (ctypes), and raise with the reason.  The
@@ -14,8 +15,10 @@ other calls, the packed projections and the cross block among them, are
 checked in Python alone.
 """
 
+import contextlib
 import ctypes
 import os
+from typing import NamedTuple
 
 import torch
 
@@ -25,11 +28,21 @@ _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.environ.get("GLIDE_LIBRARY") or os.path.join(_PKG, "libglide.so")
 
 GLIDE_OK, GLIDE_EINVAL, GLIDE_ERANGE, GLIDE_EHIP, GLIDE_ESCRATCH = 0, 1, 2, 3, 4
-GLIDE_BF16, GLIDE_F32 = 0, 1
+GLIDE_BF16, GLIDE_F32, GLIDE_E4M3, GLIDE_INT8 = 0, 1, 2, 3
+Q8_BLOCK, Q8_BLOCK_BYTES, Q8_TAIL = 32, 8192, 128
 MAX_NODES, MAX_SPLITS, HEAD_DIM, CAPE_MAX_K = 64, 64, 128, 7
 
 _lib = None
 _native = None
+
+
+class _RopeRows(ctypes.Structure):
+    _fields_ = [("inp", ctypes.c_void_p), ("out", ctypes.c_void_p), ("in_strides", ctypes.c_int64 * 3),
+                ("out_strides", ctypes.c_int64 * 3), ("H", ctypes.c_int)]
+
+
+class _Q8Pointers(ctypes.Structure):
+    _fields_ = [("blocks", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("tail", ctypes.c_void_p)]
 
 
 class GlideError(RuntimeError):
@@ -91,6 +104,23 @@ def load():
     lib.spec_sample_verify.argtypes = [P, P, P, P, I, I, I, P, P, P]
     lib.glide_expected_speedup.restype = ctypes.c_double
     lib.glide_expected_speedup.argtypes = [ctypes.c_double, I, ctypes.c_double]
+    L = ctypes.c_int64
+    lib.glide_rope.restype = I
+    lib.glide_rope.argtypes = [P, P, P, I, F, P, P, P, I, I, I, I, I, P]
+    lib.glide_rope_frequencies.restype = I
+    lib.glide_rope_frequencies.argtypes = [I, ctypes.c_double, I, ctypes.c_double, I, P, P]
+    lib.glide_q8_append.restype = I
+    lib.glide_q8_append.argtypes = [P, P, L, L, L, P, P, I, P, I, I, I, I, I, I, P]
+    lib.glide_q8_read.restype = I
+    lib.glide_q8_read.argtypes = [P, P, P, P, I, I, I, I, I, I, I, I, P]
+    lib.glide_q8_tree_attn_workspace.restype = Z
+    lib.glide_q8_tree_attn_workspace.argtypes = [I, I, I, I, I, I, I]
+    lib.glide_q8_tree_attn.restype = I
+    lib.glide_q8_tree_attn.argtypes = [P, P, P, P, P, I, I, I, I, I, I, I, F, I, P, Z, P]
+    lib.glide_q8_commit.restype = I
+    lib.glide_q8_commit.argtypes = [P, I, P, P, P, P, I, I, I, I, I, I, P]
+    lib.glide_capture_id.restype = ctypes.c_ulonglong
+    lib.glide_capture_id.argtypes = [P]
     lib.glide_verify_commit.restype = I
     lib.glide_verify_commit.argtypes = [P, I, P, P, I, I, P, P, I, I, I, I, I, P, P, P, P, P, P, P,
                                         P]
@@ -112,6 +142,9 @@ def _bind():
             lib.glide_tree_attn_workspace, lib.glide_tree_attn, lib.glide_verify_commit,
             lib.cape_expand_workspace, lib.cape_expand, lib.spec_sample_verify, lib.glide_rows_matmul,
             lib.glide_block_attn)), _raw_stream, _ws_cache)
+        native.bind_q8(tuple(ctypes.cast(f, ctypes.c_void_p).value for f in (
+            lib.glide_capture_id, lib.glide_rope, lib.glide_q8_append, lib.glide_q8_read,
+            lib.glide_q8_tree_attn_workspace, lib.glide_q8_tree_attn, lib.glide_q8_commit)))
         _native = native
     return _native
 
@@ -132,7 +165,9 @@ EXPORTED = ["glide_strerror", "glide_last_hip_error", "glide_tree_attn_workspace
             "glide_cross_block_workspace", "glide_cross_block", "glide_cross_block_packed",
             "glide_block_attn",
             "spec_sample_verify",
-            "glide_expected_speedup"]
+            "glide_expected_speedup",
+            "glide_rope", "glide_rope_frequencies", "glide_q8_append", "glide_q8_read",
+            "glide_q8_tree_attn_workspace", "glide_q8_tree_attn", "glide_q8_commit", "glide_capture_id"]
 
 
 def _ptr(t):
@@ -582,3 +617,332 @@ def _glide_block_attn(q, k_cache, v_cache, out, block, scale, stream):
                                      _stream(stream, q.device))
     _check("glide_block_attn", status)
     return out
+
+
+# ---------------------------------------------------------------------------
+# Rotary positions and a key/value cache held in 8 bits
+# ---------------------------------------------------------------------------
+
+def _on(device):
+    """The device made current for a call, if it is not."""
+    if device.index is None or device.index == torch.cuda.current_device():
+        return contextlib.nullcontext()
+    return torch.cuda.device(device)
+
+
+def _with(device, *named):
+    for name, t in named:
+        _need(t is None or t.device == device, "%s must be on %s like the others" % (name, device))
+
+
+def _row_strides(t, name):
+    """Element strides of a [B, T, H, 128] tensor; dims of size 1 have none."""
+    _need(t.dim() == 4 and t.shape[3] == HEAD_DIM, "%s must be [B, T, H, %d]" % (name, HEAD_DIM))
+    _need(t.stride(3) == 1, "%s must have its last dimension in one piece" % name)
+    return (ctypes.c_int64 * 3)(*[t.stride(i) if t.shape[i] > 1 else 0 for i in range(3)])
+
+
+def _rows_apart(t):
+    """Whether no two elements share memory: with the dims sorted by stride, each
+    steps over all that the smaller ones reach."""
+    reach = 1
+    for stride, size in sorted((t.stride(i), t.shape[i]) for i in range(t.dim()) if t.shape[i] > 1):
+        if stride < reach:
+            return False
+        reach += (size - 1) * stride
+    return True
+
+
+ROPE_SCALINGS = (None, "linear", "ntk", "yarn")
+
+
+def rope_frequencies(rot_dim, base=10000.0, scaling=None, factor=1.0, original_len=0, device="cuda"):
+    """(freqs, mscale) for glide_rope: the angles per position of the rot_dim / 2
+    pairs, float64 on `device`, and the factor of the rotated dims.  scaling:
+    None, "linear", "ntk" or "yarn" for contexts `factor` times longer than the
+    original_len trained for; see include/glide.h."""
+    _need(scaling in ROPE_SCALINGS, "scaling must be one of %s" % (ROPE_SCALINGS,))
+    _need(2 <= int(rot_dim) <= HEAD_DIM and int(rot_dim) % 2 == 0, "rot_dim must be even, 2 to %d" % HEAD_DIM)
+    freqs, mscale = (ctypes.c_double * (int(rot_dim) // 2))(), ctypes.c_float()
+    status = load().glide_rope_frequencies(int(rot_dim), float(base), ROPE_SCALINGS.index(scaling), float(factor),
+                                           int(original_len), freqs, ctypes.byref(mscale))
+    _check("glide_rope_frequencies", status)
+    return torch.tensor(list(freqs), dtype=torch.float64, device=device), mscale.value
+
+
+def glide_rope(q, k, freqs, q_out, k_out, positions=None, seq_lens=None, tree_parents=None, interleaved=False,
+               mscale=1.0, backward=False, stream=None):
+    """Rotary positions of q [B, T, H, D] and k [B, T, H_kv, D] (or None) into
+    q_out and k_out (which may be q and k), bfloat16 or float32; rows may be
+    strided.  Row t of sequence b is at positions[b, t], or at seq_lens[b] (0
+    without) plus t, or plus node t's depth in tree_parents.  backward=True
+    takes gradients of the outputs to gradients of the inputs.  See
+    include/glide.h."""
+    status = (_native or _bind()).rope(q, k, freqs, q_out, k_out, positions, seq_lens, tree_parents, interleaved,
+                                       mscale, backward, stream)
+    if status is None:
+        return _glide_rope(q, k, freqs, q_out, k_out, positions, seq_lens, tree_parents, interleaved, mscale,
+                           backward, stream)
+    _check("glide_rope", status)
+    return q_out, k_out
+
+
+def _rope_rows(x, out, name, dtype):
+    for what, t in ((name, x), (name + "_out", out)):
+        _need(isinstance(t, torch.Tensor) and t.is_cuda, "%s must be a torch tensor on the GPU" % what)
+        _need(t.dtype == dtype, "%s must be %s" % (what, dtype))
+    r = _RopeRows(x.data_ptr(), out.data_ptr(), _row_strides(x, name), _row_strides(out, name + "_out"), x.shape[2])
+    _need(out.shape == x.shape, "%s_out must match %s" % (name, name))
+    _need(_rows_apart(out), "%s_out must hold its rows apart" % name)
+    size = x.element_size()
+    for what, t, strides in ((name, x, r.in_strides), (name + "_out", out, r.out_strides)):
+        _need(t.data_ptr() % 16 == 0 and all(s * size % 16 == 0 for s in strides),
+              "%s must have its rows at multiples of 16 bytes" % what)
+    return r
+
+
+def _glide_rope(q, k, freqs, q_out, k_out, positions, seq_lens, tree_parents, interleaved, mscale, backward, stream):
+    _need(isinstance(q, torch.Tensor) and q.dtype in (torch.bfloat16, torch.float32),
+          "q must be a bfloat16 or float32 tensor")
+    rows = _rope_rows(q, q_out, "q", q.dtype)
+    B, T = q.shape[:2]
+    _need((k is None) == (k_out is None), "k and k_out must be given together")
+    keys = None
+    if k is not None:
+        keys = _rope_rows(k, k_out, "k", q.dtype)
+        _need(k.shape[:2] == (B, T), "k must be [B, T, H_kv, D] like q")
+    _dev(freqs, "freqs", torch.float64)
+    _need(freqs.dim() == 1 and 1 <= freqs.shape[0] <= HEAD_DIM // 2, "freqs must be [rot_dim / 2]")
+    for name, t, shape in (("positions", positions, (B, T)), ("seq_lens", seq_lens, (B,)),
+                           ("tree_parents", tree_parents, (B, T))):
+        if t is not None:
+            _dev(t, name, torch.int32)
+            _need(tuple(t.shape) == shape, "%s must be %s" % (name, shape))
+    _need(positions is None or (seq_lens is None and tree_parents is None),
+          "positions must be given without seq_lens and tree_parents")
+    _need(tree_parents is None or T <= MAX_NODES, "a tree has at most %d nodes" % MAX_NODES)
+    _with(q.device, ("q_out", q_out), ("k", k), ("k_out", k_out), ("freqs", freqs), ("positions", positions),
+          ("seq_lens", seq_lens), ("tree_parents", tree_parents))
+    flags = (1 if interleaved else 0) | (2 if backward else 0)
+    with _on(q.device):
+        status = load().glide_rope(
+            ctypes.byref(rows), None if keys is None else ctypes.byref(keys), _ptr(freqs), 2 * freqs.shape[0],
+            float(mscale), _ptr(positions), _ptr(seq_lens), _ptr(tree_parents), B, T, HEAD_DIM,
+            GLIDE_BF16 if q.dtype == torch.bfloat16 else GLIDE_F32, flags, _stream(stream, q.device))
+    _check("glide_rope", status)
+    return q_out, k_out
+
+
+class Q8Cache(NamedTuple):
+    """One layer's cache in 8 bits (glide_q8_cache in include/glide.h): blocks
+    [B, H_kv, L_cap / 32, 8192] float8_e4m3fn or uint8, scales [B, H_kv,
+    L_cap / 32, 2] float32, tail [B, H_kv, 2, 128, 128] bfloat16."""
+    blocks: torch.Tensor
+    scales: torch.Tensor
+    tail: torch.Tensor
+
+
+Q8_KINDS = {"e4m3": torch.float8_e4m3fn, "int8": torch.uint8}
+
+
+def q8_cache(B, H_kv, L_cap, kind="e4m3", device="cuda"):
+    """A new cache for B sequences of up to L_cap tokens (rounded up to whole
+    blocks), in 8-bit floating point ("e4m3") or integers ("int8")."""
+    _need(kind in Q8_KINDS, "kind must be one of %s" % (tuple(Q8_KINDS),))
+    n = -(-int(L_cap) // Q8_BLOCK)
+    _need(B >= 1 and H_kv >= 1 and n >= 1, "B, H_kv and L_cap must be at least 1")
+    return Q8Cache(torch.empty((B, H_kv, n, Q8_BLOCK_BYTES), dtype=Q8_KINDS[kind], device=device),
+                   torch.empty((B, H_kv, n, 2), dtype=torch.float32, device=device),
+                   torch.empty((B, H_kv, 2, Q8_TAIL, HEAD_DIM), dtype=torch.bfloat16, device=device))
+
+
+def _q8(cache):
+    """(pointers, B, H_kv, L_cap, kind, device) of a checked cache."""
+    _need(isinstance(cache, tuple) and len(cache) == 3, "a cache must be a Q8Cache (blocks, scales, tail)")
+    blocks, scales, tail = cache
+    _dev(blocks, "cache.blocks")
+    _need(blocks.dtype in Q8_KINDS.values(), "cache.blocks must be float8_e4m3fn or uint8")
+    _need(blocks.dim() == 4 and blocks.shape[3] == Q8_BLOCK_BYTES,
+          "cache.blocks must be [B, H_kv, L_cap / 32, %d]" % Q8_BLOCK_BYTES)
+    B, H, n = blocks.shape[:3]
+    _dev(scales, "cache.scales", torch.float32)
+    _need(tuple(scales.shape) == (B, H, n, 2), "cache.scales must be [B, H_kv, L_cap / 32, 2]")
+    _dev(tail, "cache.tail", torch.bfloat16)
+    _need(tuple(tail.shape) == (B, H, 2, Q8_TAIL, HEAD_DIM),
+          "cache.tail must be [B, H_kv, 2, %d, %d]" % (Q8_TAIL, HEAD_DIM))
+    _with(blocks.device, ("cache.scales", scales), ("cache.tail", tail))
+    kind = GLIDE_INT8 if blocks.dtype == torch.uint8 else GLIDE_E4M3
+    return (_Q8Pointers(blocks.data_ptr(), scales.data_ptr(), tail.data_ptr()), B, H, n * Q8_BLOCK, kind,
+            blocks.device)
+
+
+def _lens(t, name, B, device):
+    _dev(t, name, torch.int32)
+    _need(tuple(t.shape) == (B,), "%s must be [B]" % name)
+    _with(device, (name, t))
+
+
+def glide_q8_append(k_new, v_new, cache, seq_lens, counts=None, hold=False, stream=None):
+    """Writes rows k_new, v_new [B, T, H_kv, D] bfloat16 (which may be strided
+    alike) behind the seq_lens tokens of the cache: final rows, or with
+    hold=True a tree's, to be verified.  seq_lens is not changed.  See
+    include/glide.h."""
+    status = (_native or _bind()).q8_append(k_new, v_new, cache, seq_lens, counts, hold, stream)
+    if status is None:
+        return _glide_q8_append(k_new, v_new, cache, seq_lens, counts, hold, stream)
+    _check("glide_q8_append", status)
+    return cache
+
+
+def _glide_q8_append(k_new, v_new, cache, seq_lens, counts, hold, stream):
+    c, B, H, L_cap, kind, device = _q8(cache)
+    strides = []
+    for name, t in (("k_new", k_new), ("v_new", v_new)):
+        _need(isinstance(t, torch.Tensor) and t.is_cuda, "%s must be a torch tensor on the GPU" % name)
+        _need(t.dtype == torch.bfloat16, "%s must be bfloat16" % name)
+        strides.append(_row_strides(t, name))
+        _need(t.shape[0] == B and t.shape[2] == H, "%s must be [B, T, H_kv, D]" % name)
+        _need(t.data_ptr() % 16 == 0 and all(s % 8 == 0 for s in strides[-1]),
+              "%s must have its rows at multiples of 16 bytes" % name)
+    _need(v_new.shape == k_new.shape and list(strides[0]) == list(strides[1]),
+          "v_new must match k_new, strides included")
+    T = k_new.shape[1]
+    _need(T >= 1 and (not hold or T <= MAX_NODES), "T must be at least 1, and at most %d rows are held" % MAX_NODES)
+    _lens(seq_lens, "seq_lens", B, device)
+    if counts is not None:
+        _lens(counts, "counts", B, device)
+    _with(device, ("k_new", k_new), ("v_new", v_new))
+    with _on(device):
+        status = load().glide_q8_append(_ptr(k_new), _ptr(v_new), *strides[0], _ptr(seq_lens), _ptr(counts),
+                                        1 if hold else 0, ctypes.byref(c), B, T, H, HEAD_DIM, L_cap, kind,
+                                        _stream(stream, device))
+    _check("glide_q8_append", status)
+    return cache
+
+
+def glide_q8_read(cache, seq_lens, k_out, v_out, start=0, stream=None):
+    """Tokens [start, start + T) of the cache as rows of k_out and v_out [B, H_kv,
+    T, D], bfloat16 or float32; rows behind a sequence's seq_lens tokens stay as
+    they are.  See include/glide.h."""
+    status = (_native or _bind()).q8_read(cache, seq_lens, k_out, v_out, start, stream)
+    if status is None:
+        return _glide_q8_read(cache, seq_lens, k_out, v_out, start, stream)
+    _check("glide_q8_read", status)
+    return k_out, v_out
+
+
+def _glide_q8_read(cache, seq_lens, k_out, v_out, start, stream):
+    c, B, H, L_cap, kind, device = _q8(cache)
+    _dev(k_out, "k_out")
+    _need(k_out.dtype in (torch.bfloat16, torch.float32), "k_out must be bfloat16 or float32")
+    _dev(v_out, "v_out", k_out.dtype)
+    _need(k_out.dim() == 4 and k_out.shape[:2] == (B, H) and k_out.shape[3] == HEAD_DIM,
+          "k_out must be [B, H_kv, T, D]")
+    _need(v_out.shape == k_out.shape, "v_out must match k_out")
+    _lens(seq_lens, "seq_lens", B, device)
+    _with(device, ("k_out", k_out), ("v_out", v_out))
+    with _on(device):
+        status = load().glide_q8_read(ctypes.byref(c), _ptr(seq_lens), _ptr(k_out), _ptr(v_out),
+                                      GLIDE_BF16 if k_out.dtype == torch.bfloat16 else GLIDE_F32, B, H, HEAD_DIM,
+                                      L_cap, kind, int(start), k_out.shape[2], _stream(stream, device))
+    _check("glide_q8_read", status)
+    return k_out, v_out
+
+
+# Workspaces of captured calls: {(device index, stream handle): (capture, byte
+# tensor)}.  A graph's workspace is its own -- allocated and zeroed inside the
+# capture, in the memory that the graph keeps -- so that two graphs, or a graph
+# and eager calls, can run at once.  One entry a stream: the last capture's.
+_captured_ws = {}
+
+
+def q8_attn_workspace(B, N, H, H_kv, L_cap, max_splits, device, stream=None):
+    """The kept workspace of glide_q8_tree_attn for the stream (shared with
+    glide_tree_attn), or under a capture that capture's; None if none is needed."""
+    need = load().glide_q8_tree_attn_workspace(B, N, H, H_kv, HEAD_DIM, L_cap, max_splits)
+    if need == 0:
+        return None
+    s = torch.cuda.current_stream(device) if stream is None else stream
+    index = torch.device(device).index
+    key = (torch.cuda.current_device() if index is None else index, s.cuda_stream)
+    capture = load().glide_capture_id(ctypes.c_void_p(s.cuda_stream))
+    if capture:
+        held = _captured_ws.get(key)
+        if held is None or held[0] != capture or held[1].numel() < need:
+            held = _captured_ws[key] = (capture, _alloc_bytes(need, device, s, zero=True))
+        return held[1]
+    ws = _ws_cache.get(key)
+    if ws is None or ws.numel() < need:
+        ws = _ws_cache[key] = _alloc_bytes(need, device, s, zero=True)
+    return ws
+
+
+def glide_q8_tree_attn(q, cache, seq_lens, tree_parents, out, scale=0.0, max_splits=0, workspace=None, stream=None):
+    """glide_tree_attn over an 8-bit cache, with H / H_kv query heads to a cached
+    head: q, out [B, N, H, D] bfloat16.  See include/glide.h."""
+    status = (_native or _bind()).q8_tree_attn(q, cache, seq_lens, tree_parents, out, scale, max_splits, workspace,
+                                               stream)
+    if status is None:
+        return _glide_q8_tree_attn(q, cache, seq_lens, tree_parents, out, scale, max_splits, workspace, stream)
+    _check("glide_q8_tree_attn", status)
+    return out
+
+
+def _glide_q8_tree_attn(q, cache, seq_lens, tree_parents, out, scale, max_splits, workspace, stream):
+    c, B, H_kv, L_cap, kind, device = _q8(cache)
+    _dev(q, "q", torch.bfloat16)
+    _dev(out, "out", torch.bfloat16)
+    _need(q.dim() == 4 and q.shape[0] == B and q.shape[3] == HEAD_DIM, "q must be [B, N, H, D]")
+    _need(out.shape == q.shape, "out must match q")
+    N, H = q.shape[1:3]
+    _need(H >= H_kv and H % H_kv == 0, "q's heads must be a multiple of the cache's")
+    _lens(seq_lens, "seq_lens", B, device)
+    if tree_parents is not None:
+        _dev(tree_parents, "tree_parents", torch.int32)
+        _need(tuple(tree_parents.shape) == (B, N), "tree_parents must be [B, N]")
+    _with(device, ("q", q), ("out", out), ("tree_parents", tree_parents), ("workspace", workspace))
+    with _on(device):
+        if workspace is None:
+            workspace = q8_attn_workspace(B, N, H, H_kv, L_cap, int(max_splits), device, stream)
+        else:
+            _dev(workspace, "workspace")
+        ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+        status = load().glide_q8_tree_attn(
+            _ptr(q), ctypes.byref(c), _ptr(seq_lens), _ptr(tree_parents), _ptr(out), B, N, H, H_kv, HEAD_DIM, L_cap,
+            kind, float(scale), int(max_splits), _ptr(workspace), ws_bytes, _stream(stream, device))
+    _check("glide_q8_tree_attn", status)
+    return out
+
+
+def glide_q8_commit(caches, seq_lens, accept_len, path, seq_lens_out, nodes=None, stream=None):
+    """Commits the accepted rows of a verification step in every layer's 8-bit
+    cache and writes the new lengths.  caches: a Q8Cache per layer; path [B, N]
+    as glide_verify_commit gives it, or None for a chain (of at most `nodes`
+    rows, by default 64).  See include/glide.h."""
+    if nodes is None:
+        nodes = path.shape[1] if isinstance(path, torch.Tensor) and path.dim() == 2 else MAX_NODES
+    status = (_native or _bind()).q8_commit(caches, seq_lens, accept_len, path, seq_lens_out, nodes, stream)
+    if status is None:
+        return _glide_q8_commit(caches, seq_lens, accept_len, path, seq_lens_out, nodes, stream)
+    _check("glide_q8_commit", status)
+    return seq_lens_out
+
+
+def _glide_q8_commit(caches, seq_lens, accept_len, path, seq_lens_out, nodes, stream):
+    caches = list(caches)
+    _need(len(caches) >= 1, "caches must hold at least one layer's")
+    views = [_q8(c) for c in caches]
+    _, B, H, L_cap, kind, device = views[0]
+    _need(all(v[1:] == views[0][1:] for v in views), "every cache must be like the first")
+    for name, t in (("seq_lens", seq_lens), ("accept_len", accept_len), ("seq_lens_out", seq_lens_out)):
+        _lens(t, name, B, device)
+    if path is not None:
+        _dev(path, "path", torch.int32)
+        _need(tuple(path.shape) == (B, nodes), "path must be [B, N]")
+        _with(device, ("path", path))
+    with _on(device):
+        status = load().glide_q8_commit((_Q8Pointers * len(views))(*[v[0] for v in views]), len(views),
+                                        _ptr(seq_lens), _ptr(accept_len), _ptr(path), _ptr(seq_lens_out), B,
+                                        int(nodes), H, HEAD_DIM, L_cap, kind, _stream(stream, device))
+    _check("glide_q8_commit", status)
+    return seq_lens_out

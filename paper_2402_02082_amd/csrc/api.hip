@@ -11,6 +11,7 @@
 
 #include "glide.h"
 #include "internal.h"
+#include "q8.h"
 
 // Fixed scratch of glide_tree_attn_noalloc (see scratch_of_current_device).
 static constexpr size_t kNoAllocScratchBytes = (size_t)16 << 20;
@@ -157,6 +158,54 @@ int scratch_of_current_device(void** ptr) {
   return GLIDE_OK;
 }
 
+
+// ---------------------------------------------------------------------------
+// 8-bit caches.
+// ---------------------------------------------------------------------------
+static_assert(GLIDE_Q8_BLOCK == glide::kQ8Block && GLIDE_Q8_TAIL == glide::kQ8Tail &&
+                  GLIDE_Q8_BLOCK_BYTES == glide::kQ8BlockBytes,
+              "the header's sizes are the kernels'");
+
+bool q8_sizes_ok(int B, int H_kv, int D, int L_cap, int kind) {
+  if (B < 1 || B > 65535 || H_kv < 1 || H_kv > 65535 || D != glide::kHeadDim) return false;  // grid dims
+  if (L_cap < glide::kQ8Block || L_cap > kMaxKeys || L_cap % glide::kQ8Block) return false;
+  return kind == GLIDE_E4M3 || kind == GLIDE_INT8;
+}
+
+bool q8_cache_ok(const glide_q8_cache* c, glide::Q8Cache* out) {
+  if (!c || !c->blocks || !c->scales || !c->tail) return false;
+  if (!aligned16(c->blocks) || !aligned16(c->scales) || !aligned16(c->tail)) return false;
+  *out = glide::Q8Cache{(uint8_t*)c->blocks, c->scales, (uint16_t*)c->tail};
+  return true;
+}
+
+// Lengths (and with `more` the rows added to them) inside [0, L_cap].
+int q8_lens_check(const int32_t* seq_lens, const int32_t* more, int fixed, int most, int B, int L_cap,
+                  hipStream_t stream) {
+  int status = GLIDE_OK;
+  std::vector<int32_t> lens, add;
+  if (!fetch_ints(seq_lens, (size_t)B, lens, stream, &status)) return status;
+  if (more && !fetch_ints(more, (size_t)B, add, stream, &status)) return status;
+  for (int b = 0; b < B; ++b) {
+    const int n = more ? add[b] : fixed;
+    if (lens[b] < 0 || lens[b] > L_cap || n < 0 || n > most || n > L_cap - lens[b]) return GLIDE_ERANGE;
+  }
+  return GLIDE_OK;
+}
+
+bool q8_attn_sizes_ok(int B, int N, int H, int H_kv, int D, int L_cap) {
+  if (!q8_sizes_ok(B, H_kv, D, L_cap, GLIDE_E4M3)) return false;
+  if (N < 1 || N > glide::kMaxNodes || H < H_kv || H % H_kv) return false;
+  return (double)B * N * H <= 2147483647.0;
+}
+
+bool rope_rows_ok(const glide_rope_rows* r, int B, int T, int elem) {
+  if (!r->in || !r->out || !aligned16(r->in) || !aligned16(r->out) || r->H < 1) return false;
+  for (int i = 0; i < 3; ++i)
+    if (r->in_strides[i] < 0 || r->out_strides[i] < 0 || r->in_strides[i] * elem % 16 || r->out_strides[i] * elem % 16)
+      return false;
+  return true;
+}
 
 // Shared body of glide_tree_attn and glide_tree_attn_noalloc.  With
 // `scratch` set, the split partials go to the per-device scratch array that
@@ -445,6 +494,208 @@ int spec_sample_verify(const int32_t* draft_tokens, const float* draft_probs, co
   if ((double)B * (gamma + 1) * V > 9.0e18) return GLIDE_EINVAL;
   return hip_status(glide::launch_spec_sample(draft_tokens, draft_probs, target_probs, uniforms, B, gamma,
                                               V, accept_len, next_token, stream));
+}
+
+int glide_rope(const glide_rope_rows* q, const glide_rope_rows* k, const double* freqs, int rot_dim,
+               float mscale, const int32_t* positions, const int32_t* seq_lens,
+               const int32_t* tree_parents, int B, int T, int D, int dtype, int flags,
+               hipStream_t stream) {
+  if (!q || !freqs || (dtype != GLIDE_BF16 && dtype != GLIDE_F32)) return GLIDE_EINVAL;
+  const int elem = dtype == GLIDE_BF16 ? 2 : 4;
+  if (B < 1 || B > 65535 || T < 1 || D != glide::kHeadDim) return GLIDE_EINVAL;
+  if (!rope_rows_ok(q, B, T, elem) || (k && !rope_rows_ok(k, B, T, elem))) return GLIDE_EINVAL;
+  if (rot_dim < 2 || rot_dim > D || rot_dim % 2 || !isfinite(mscale)) return GLIDE_EINVAL;
+  if (flags & ~(GLIDE_ROPE_INTERLEAVED | GLIDE_ROPE_BACKWARD)) return GLIDE_EINVAL;
+  if (positions && (seq_lens || tree_parents)) return GLIDE_EINVAL;
+  if (tree_parents && T > glide::kMaxNodes) return GLIDE_EINVAL;
+  if ((double)B * T * ((double)q->H + (k ? k->H : 0)) > 2147483647.0) return GLIDE_EINVAL;
+  if (validate_enabled() && tree_parents) {
+    int status = GLIDE_OK;
+    std::vector<int32_t> par;
+    if (!fetch_ints(tree_parents, (size_t)B * T, par, stream, &status)) return status;
+    if (!parents_ok(par, B, T)) return GLIDE_ERANGE;
+  }
+  auto rows = [](const glide_rope_rows& r) {
+    return glide::RopeRows{r.in, r.out, r.in_strides[0], r.in_strides[1], r.in_strides[2],
+                           r.out_strides[0], r.out_strides[1], r.out_strides[2], r.H};
+  };
+  glide::RopeArgs a{};
+  a.q = rows(*q);
+  if (k) a.k = rows(*k);
+  a.freqs = freqs;
+  a.positions = positions;
+  a.seq_lens = seq_lens;
+  a.parents = tree_parents;
+  a.B = B;
+  a.T = T;
+  a.rot = rot_dim;
+  a.mscale = mscale;
+  return hip_status(glide::launch_rope(a, dtype == GLIDE_BF16, flags & GLIDE_ROPE_INTERLEAVED,
+                                       flags & GLIDE_ROPE_BACKWARD, stream));
+}
+
+int glide_rope_frequencies(int rot_dim, double base, int scaling, double factor, int original_len,
+                           double* freqs, float* mscale) {
+  if (!freqs || !mscale || rot_dim < 2 || rot_dim > glide::kHeadDim || rot_dim % 2) return GLIDE_EINVAL;
+  if (!(base > 1.0) || !isfinite(base) || !(factor >= 1.0) || !isfinite(factor)) return GLIDE_EINVAL;
+  if (scaling < GLIDE_ROPE_PLAIN || scaling > GLIDE_ROPE_YARN) return GLIDE_EINVAL;
+  if (scaling == GLIDE_ROPE_NTK && rot_dim < 4) return GLIDE_EINVAL;
+  if (scaling == GLIDE_ROPE_YARN && original_len < 1) return GLIDE_EINVAL;
+  if (scaling == GLIDE_ROPE_NTK) base *= pow(factor, rot_dim / (rot_dim - 2.0));
+  if (!isfinite(base)) return GLIDE_EINVAL;
+  for (int i = 0; i < rot_dim / 2; ++i) {
+    double f = pow(base, -2.0 * i / rot_dim);
+    if (scaling == GLIDE_ROPE_LINEAR) f /= factor;
+    if (scaling == GLIDE_ROPE_YARN) {
+      const double turns = original_len * f / 6.283185307179586477;
+      const double keep = fmin(1.0, fmax(0.0, (turns - 1.0) / 31.0));
+      f = f * keep + f / factor * (1.0 - keep);
+    }
+    freqs[i] = f;
+  }
+  *mscale = scaling == GLIDE_ROPE_YARN ? (float)(0.1 * log(factor) + 1.0) : 1.f;
+  return GLIDE_OK;
+}
+
+int glide_q8_append(const void* k_new, const void* v_new, int64_t stride_b, int64_t stride_t,
+                    int64_t stride_h, const int32_t* seq_lens, const int32_t* counts, int hold,
+                    const glide_q8_cache* cache, int B, int T, int H_kv, int D, int L_cap, int kind,
+                    hipStream_t stream) {
+  glide::Q8AppendArgs a{};
+  if (!k_new || !v_new || !aligned16(k_new) || !aligned16(v_new) || !seq_lens) return GLIDE_EINVAL;
+  if (!q8_sizes_ok(B, H_kv, D, L_cap, kind) || !q8_cache_ok(cache, &a.cache)) return GLIDE_EINVAL;
+  if (T < 1 || T > kMaxKeys || (hold && T > glide::kMaxNodes)) return GLIDE_EINVAL;
+  for (const int64_t s : {stride_b, stride_t, stride_h})
+    if (s < 0 || s % 8) return GLIDE_EINVAL;
+  if (validate_enabled()) {
+    const int st = hold ? q8_lens_check(seq_lens, nullptr, 0, 0, B, L_cap, stream)
+                        : q8_lens_check(seq_lens, counts, T, T, B, L_cap, stream);
+    if (st != GLIDE_OK) return st;
+  }
+  a.k = (const uint16_t*)k_new;
+  a.v = (const uint16_t*)v_new;
+  a.seq_lens = seq_lens;
+  a.counts = counts;
+  a.sb = stride_b;
+  a.st = stride_t;
+  a.sh = stride_h;
+  a.B = B;
+  a.T = T;
+  a.H = H_kv;
+  a.n_blocks = L_cap / glide::kQ8Block;
+  return hip_status(glide::launch_q8_append(a, kind == GLIDE_INT8, hold != 0, stream));
+}
+
+int glide_q8_read(const glide_q8_cache* cache, const int32_t* seq_lens, void* k_out, void* v_out,
+                  int out_dtype, int B, int H_kv, int D, int L_cap, int kind, int start, int T,
+                  hipStream_t stream) {
+  glide::Q8ReadArgs a{};
+  if (!seq_lens || !k_out || !v_out || !aligned16(k_out) || !aligned16(v_out)) return GLIDE_EINVAL;
+  if (!q8_sizes_ok(B, H_kv, D, L_cap, kind) || !q8_cache_ok(cache, &a.cache)) return GLIDE_EINVAL;
+  if (out_dtype != GLIDE_BF16 && out_dtype != GLIDE_F32) return GLIDE_EINVAL;
+  if (start < 0 || T < 1 || (int64_t)start + T > (int64_t)L_cap + glide::kQ8Block - 1) return GLIDE_EINVAL;
+  if (validate_enabled()) {
+    const int st = q8_lens_check(seq_lens, nullptr, 0, 0, B, L_cap, stream);
+    if (st != GLIDE_OK) return st;
+  }
+  a.seq_lens = seq_lens;
+  a.k_out = k_out;
+  a.v_out = v_out;
+  a.B = B;
+  a.H = H_kv;
+  a.n_blocks = L_cap / glide::kQ8Block;
+  a.start = start;
+  a.T = T;
+  return hip_status(glide::launch_q8_read(a, kind == GLIDE_INT8, out_dtype == GLIDE_BF16, stream));
+}
+
+size_t glide_q8_tree_attn_workspace(int B, int N, int H, int H_kv, int D, int L_cap, int max_splits) {
+  if (!q8_attn_sizes_ok(B, N, H, H_kv, D, L_cap)) return 0;
+  if (max_splits < 0 || max_splits > glide::kMaxSplits) return 0;
+  return glide::plan_q8_attn(B, N, H, H_kv, L_cap / glide::kQ8Block, max_splits).ws_bytes;
+}
+
+int glide_q8_tree_attn(const void* q, const glide_q8_cache* cache, const int32_t* seq_lens,
+                       const int32_t* tree_parents, void* out, int B, int N, int H, int H_kv, int D,
+                       int L_cap, int kind, float scale, int max_splits, void* workspace,
+                       size_t ws_bytes, hipStream_t stream) {
+  glide::Q8AttnArgs a{};
+  if (!q || !seq_lens || !out || !aligned16(q) || !aligned16(out)) return GLIDE_EINVAL;
+  if (!q8_sizes_ok(B, H_kv, D, L_cap, kind) || !q8_cache_ok(cache, &a.cache)) return GLIDE_EINVAL;
+  if (!q8_attn_sizes_ok(B, N, H, H_kv, D, L_cap) || !isfinite(scale)) return GLIDE_EINVAL;
+  if (max_splits < 0 || max_splits > glide::kMaxSplits) return GLIDE_EINVAL;
+  const glide::Q8AttnPlan p = glide::plan_q8_attn(B, N, H, H_kv, L_cap / glide::kQ8Block, max_splits);
+  if (p.ws_bytes > 0 && (!workspace || !aligned16(workspace) || ws_bytes < p.ws_bytes)) return GLIDE_EINVAL;
+  if (validate_enabled()) {
+    int status = q8_lens_check(seq_lens, nullptr, 0, 0, B, L_cap, stream);
+    std::vector<int32_t> par;
+    if (status != GLIDE_OK) return status;
+    if (tree_parents) {
+      if (!fetch_ints(tree_parents, (size_t)B * N, par, stream, &status)) return status;
+      if (!parents_ok(par, B, N)) return GLIDE_ERANGE;
+    }
+  }
+  a.q = (const uint16_t*)q;
+  a.seq_lens = seq_lens;
+  a.parents = tree_parents;
+  a.out = (uint16_t*)out;
+  a.part_o = p.ws_bytes ? (float*)((char*)workspace + p.part_o_off) : nullptr;
+  a.part_ml = p.ws_bytes ? (float2*)((char*)workspace + p.part_ml_off) : nullptr;
+  a.B = B;
+  a.N = N;
+  a.H = H;
+  a.H_kv = H_kv;
+  a.n_blocks = L_cap / glide::kQ8Block;
+  a.groups = p.groups;
+  a.splits = p.splits;
+  const double sc = scale > 0.f ? (double)scale : 1.0 / sqrt((double)D);
+  a.scale_log2 = (float)(sc * 1.4426950408889634);  // log2(e)
+  return hip_status(glide::launch_q8_attn(a, kind == GLIDE_INT8, p.tiles, stream));
+}
+
+int glide_q8_commit(const glide_q8_cache* caches, int layers, const int32_t* seq_lens,
+                    const int32_t* accept_len, const int32_t* path, int32_t* seq_lens_out, int B,
+                    int N, int H_kv, int D, int L_cap, int kind, hipStream_t stream) {
+  glide::Q8CommitArgs a{};
+  if (!caches || !seq_lens || !accept_len || !seq_lens_out || seq_lens_out == seq_lens) return GLIDE_EINVAL;
+  if (layers < 1 || layers > glide::kQ8MaxLayers || N < 1 || N > glide::kMaxNodes) return GLIDE_EINVAL;
+  if (!q8_sizes_ok(B, H_kv, D, L_cap, kind)) return GLIDE_EINVAL;
+  for (int l = 0; l < layers; ++l)
+    if (!q8_cache_ok(&caches[l], &a.cache[l])) return GLIDE_EINVAL;
+  if (validate_enabled()) {
+    int status = q8_lens_check(seq_lens, accept_len, 0, N, B, L_cap, stream);
+    if (status != GLIDE_OK) return status;
+    if (path) {
+      std::vector<int32_t> nodes, acc;
+      if (!fetch_ints(path, (size_t)B * N, nodes, stream, &status)) return status;
+      if (!fetch_ints(accept_len, (size_t)B, acc, stream, &status)) return status;
+      for (int b = 0; b < B; ++b)
+        for (int d = 0; d < acc[b]; ++d) {
+          const int n = nodes[(size_t)b * N + d], before = d ? nodes[(size_t)b * N + d - 1] : -1;
+          if (n <= before || n >= N) return GLIDE_ERANGE;
+        }
+    }
+  }
+  a.seq_lens = seq_lens;
+  a.accept_len = accept_len;
+  a.path = path;
+  a.seq_lens_out = seq_lens_out;
+  a.B = B;
+  a.H = H_kv;
+  a.N = N;
+  a.n_blocks = L_cap / glide::kQ8Block;
+  a.layers = layers;
+  return hip_status(glide::launch_q8_commit(a, kind == GLIDE_INT8, stream));
+}
+
+unsigned long long glide_capture_id(hipStream_t stream) {
+  hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
+  unsigned long long id = 0;
+  if (hipStreamGetCaptureInfo(stream, &status, &id) != hipSuccess) {
+    (void)hipGetLastError();  // not the next launch's error
+    return 0;
+  }
+  return status == hipStreamCaptureStatusActive ? id : 0;
 }
 
 double glide_expected_speedup(double alpha, int gamma, double c) {

@@ -16,6 +16,9 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <ATen/ATen.h>
+#include <c10/core/impl/VirtualGuardImpl.h>
+
+#include <algorithm>
 
 #include "glide.h"
 
@@ -32,6 +35,16 @@ struct Calls {
   decltype(&glide_rows_matmul) rows_matmul;
   decltype(&glide_block_attn) block_attn;
 } calls;
+// ... and those of the rotary positions and the 8-bit cache (bind_q8()).
+struct Q8Calls {
+  decltype(&glide_capture_id) capture_id;
+  decltype(&glide_rope) rope;
+  decltype(&glide_q8_append) append;
+  decltype(&glide_q8_read) read;
+  decltype(&glide_q8_tree_attn_workspace) attn_workspace;
+  decltype(&glide_q8_tree_attn) attn;
+  decltype(&glide_q8_commit) commit;
+} q8;
 PyObject* raw_stream;  // device index -> current stream handle
 PyObject* workspaces;  // {(device index, stream handle): byte tensor}
 
@@ -305,6 +318,250 @@ PyObject* block_attn(PyObject* const* a, Py_ssize_t n) {
   return status_of([&] { return calls.block_attn(qp, kp, vp, op, B, T, H, D, cap, block, scale, s); });
 }
 
+// ---------------------------------------------------------------------------
+// Rotary positions and the 8-bit cache: every tensor on the current device.
+// ---------------------------------------------------------------------------
+bool on_current(const at::Tensor& t) {
+  static const c10::impl::VirtualGuardImpl guard(at::kCUDA);
+  return t.is_cuda() && t.device() == guard.getDevice();
+}
+
+// A contiguous tensor of the type on the device of `on`.
+const at::Tensor* there(PyObject* o, at::ScalarType dtype, const at::Tensor& on) {
+  const at::Tensor* t = gpu(o, dtype, -1);
+  return t && t->device() == on.device() ? t : nullptr;
+}
+
+// An optional one of the given shape: false if it is something else.
+bool optional_there(PyObject* o, at::ScalarType dtype, at::IntArrayRef shape, const at::Tensor& on,
+                    const at::Tensor** t) {
+  *t = nullptr;
+  if (o == Py_None) return true;
+  *t = there(o, dtype, on);
+  return *t && is_shape(**t, shape);
+}
+
+// Element strides of a [B, T, H, 128] tensor whose rows are in one piece;
+// dims of size 1 have none.
+bool row_strides(const at::Tensor& t, int64_t* s) {
+  if (t.dim() != 4 || t.size(3) != GLIDE_HEAD_DIM || t.stride(3) != 1) return false;
+  for (int i = 0; i < 3; ++i) s[i] = t.size(i) > 1 ? t.stride(i) : 0;
+  return true;
+}
+
+// Rows that are written must be apart from each other: with the dims sorted by
+// stride, each steps over all that the smaller ones reach.
+bool rows_apart(const int64_t* s, const at::Tensor& t) {
+  int order[3] = {0, 1, 2};
+  std::sort(order, order + 3, [&](int a, int b) { return s[a] < s[b]; });
+  int64_t reach = GLIDE_HEAD_DIM;
+  for (int i : order) {
+    if (t.size(i) <= 1) continue;
+    if (s[i] < reach) return false;
+    reach += (t.size(i) - 1) * s[i];
+  }
+  return true;
+}
+
+bool rope_rows(PyObject* in, PyObject* out, const at::Tensor** x, const at::Tensor** y, glide_rope_rows* r) {
+  *x = tensor(in), *y = tensor(out);
+  if (!*x || !*y || (*x)->sizes() != (*y)->sizes() || (*x)->scalar_type() != (*y)->scalar_type() || !fits(**x))
+    return false;
+  if ((*x)->device() != (*y)->device() || !row_strides(**x, r->in_strides) || !row_strides(**y, r->out_strides))
+    return false;
+  if (!rows_apart(r->out_strides, **y)) return false;
+  r->in = (*x)->data_ptr();
+  r->out = (*y)->data_ptr();
+  r->H = (*x)->size(2);
+  return true;
+}
+
+// (q, k, freqs, q_out, k_out, positions, seq_lens, tree_parents, interleaved, mscale, backward, stream)
+PyObject* rope(PyObject* const* a, Py_ssize_t n) {
+  if (n != 12 || a[11] != Py_None || !PyBool_Check(a[8]) || !PyBool_Check(a[10])) return nullptr;
+  const at::Tensor *q, *qo, *k, *ko;
+  glide_rope_rows rq, rk;
+  if (!rope_rows(a[0], a[3], &q, &qo, &rq) || !on_current(*q)) return nullptr;
+  const auto dtype = q->scalar_type();
+  if (dtype != kBf16 && dtype != kF32) return nullptr;
+  const int64_t B = q->size(0), T = q->size(1);
+  const bool keys = a[1] != Py_None;
+  if (keys) {
+    if (!rope_rows(a[1], a[4], &k, &ko, &rk) || k->scalar_type() != dtype || k->device() != q->device() ||
+        k->size(0) != B || k->size(1) != T)
+      return nullptr;
+  } else if (a[4] != Py_None) {
+    return nullptr;
+  }
+  const at::Tensor *freqs = there(a[2], at::kDouble, *q), *pos, *lens, *parents;
+  if (!freqs || freqs->dim() != 1 || freqs->size(0) > GLIDE_HEAD_DIM / 2) return nullptr;
+  if (!optional_there(a[5], kI32, {B, T}, *q, &pos) || !optional_there(a[6], kI32, {B}, *q, &lens) ||
+      !optional_there(a[7], kI32, {B, T}, *q, &parents))
+    return nullptr;
+  float m;
+  hipStream_t s;
+  if (!as_float(a[9], &m) || !stream_of(*q, &s, nullptr)) return nullptr;
+  const int flags = (a[8] == Py_True ? GLIDE_ROPE_INTERLEAVED : 0) | (a[10] == Py_True ? GLIDE_ROPE_BACKWARD : 0);
+  const double* f = (const double*)ptr(freqs);
+  const int rot = 2 * freqs->size(0);
+  const int32_t *pp = (const int32_t*)ptr(pos), *lp = (const int32_t*)ptr(lens), *tp = (const int32_t*)ptr(parents);
+  return status_of([&] {
+    return q8.rope(&rq, keys ? &rk : nullptr, f, rot, m, pp, lp, tp, B, T, GLIDE_HEAD_DIM,
+                   dtype == kBf16 ? GLIDE_BF16 : GLIDE_F32, flags, s);
+  });
+}
+
+// (blocks, scales, tail) of one layer, all of the same sizes.
+struct Q8View {
+  const at::Tensor* blocks;
+  glide_q8_cache c;
+  int64_t B, H, cap;
+  int kind;
+};
+
+bool q8_view(PyObject* o, Q8View* v) {
+  if (!PyTuple_Check(o) || PyTuple_GET_SIZE(o) != 3) return false;
+  const at::Tensor* blocks = tensor(PyTuple_GET_ITEM(o, 0));
+  if (!blocks || (blocks->scalar_type() != at::kByte && blocks->scalar_type() != at::kFloat8_e4m3fn)) return false;
+  blocks = gpu(PyTuple_GET_ITEM(o, 0), blocks->scalar_type(), 4);
+  if (!blocks || blocks->size(3) != GLIDE_Q8_BLOCK_BYTES || !fits(*blocks)) return false;
+  v->blocks = blocks;
+  v->B = blocks->size(0), v->H = blocks->size(1), v->cap = blocks->size(2) * GLIDE_Q8_BLOCK;
+  v->kind = blocks->scalar_type() == at::kByte ? GLIDE_INT8 : GLIDE_E4M3;
+  const at::Tensor *scales = there(PyTuple_GET_ITEM(o, 1), kF32, *blocks), *tail = there(PyTuple_GET_ITEM(o, 2), kBf16, *blocks);
+  if (!scales || !tail || v->cap > INT32_MAX || !is_shape(*scales, {v->B, v->H, blocks->size(2), 2}) ||
+      !is_shape(*tail, {v->B, v->H, 2, GLIDE_Q8_TAIL, GLIDE_HEAD_DIM}))
+    return false;
+  v->c = glide_q8_cache{blocks->data_ptr(), (float*)scales->data_ptr(), tail->data_ptr()};
+  return true;
+}
+
+// (k_new, v_new, cache, seq_lens, counts, hold, stream)
+PyObject* q8_append(PyObject* const* a, Py_ssize_t n) {
+  Q8View c;
+  if (n != 7 || a[6] != Py_None || !PyBool_Check(a[5]) || !q8_view(a[2], &c) || !on_current(*c.blocks)) return nullptr;
+  const at::Tensor *k = tensor(a[0]), *v = tensor(a[1]), *lens = there(a[3], kI32, *c.blocks), *counts;
+  int64_t ks[3], vs[3];
+  if (!k || !v || !lens || k->scalar_type() != kBf16 || v->scalar_type() != kBf16 || !fits(*k) ||
+      k->device() != c.blocks->device() || v->device() != c.blocks->device() || v->sizes() != k->sizes() ||
+      !row_strides(*k, ks) || !row_strides(*v, vs) || memcmp(ks, vs, sizeof(ks)))
+    return nullptr;
+  const int64_t T = k->size(1);
+  if (k->size(0) != c.B || k->size(2) != c.H || !is_shape(*lens, {c.B}) ||
+      !optional_there(a[4], kI32, {c.B}, *c.blocks, &counts))
+    return nullptr;
+  hipStream_t s;
+  if (!stream_of(*k, &s, nullptr)) return nullptr;
+  const bool hold = a[5] == Py_True;
+  const void *kp = k->data_ptr(), *vp = v->data_ptr();
+  const int32_t *lp = (const int32_t*)ptr(lens), *cp = (const int32_t*)ptr(counts);
+  return status_of([&] {
+    return q8.append(kp, vp, ks[0], ks[1], ks[2], lp, cp, hold, &c.c, c.B, T, c.H, GLIDE_HEAD_DIM, c.cap, c.kind, s);
+  });
+}
+
+// (cache, seq_lens, k_out, v_out, start, stream)
+PyObject* q8_read(PyObject* const* a, Py_ssize_t n) {
+  Q8View c;
+  int start;
+  if (n != 6 || a[5] != Py_None || !q8_view(a[0], &c) || !on_current(*c.blocks) || !as_int(a[4], &start)) return nullptr;
+  const at::Tensor *lens = there(a[1], kI32, *c.blocks), *k = tensor(a[2]), *v;
+  if (!lens || !k || (k->scalar_type() != kBf16 && k->scalar_type() != kF32)) return nullptr;
+  const auto dtype = k->scalar_type();
+  k = there(a[2], dtype, *c.blocks), v = there(a[3], dtype, *c.blocks);
+  if (!k || !v || k->dim() != 4 || !fits(*k) || !is_shape(*k, {c.B, c.H, k->size(2), GLIDE_HEAD_DIM}) ||
+      v->sizes() != k->sizes() || !is_shape(*lens, {c.B}))
+    return nullptr;
+  hipStream_t s;
+  if (!stream_of(*k, &s, nullptr)) return nullptr;
+  const int32_t* lp = (const int32_t*)ptr(lens);
+  void *kp = ptr(k), *vp = ptr(v);
+  const int64_t T = k->size(2);
+  return status_of([&] {
+    return q8.read(&c.c, lp, kp, vp, dtype == kBf16 ? GLIDE_BF16 : GLIDE_F32, c.B, c.H, GLIDE_HEAD_DIM, c.cap, c.kind,
+                   start, T, s);
+  });
+}
+
+// (q, cache, seq_lens, tree_parents, out, scale, max_splits, workspace, stream)
+PyObject* q8_tree_attn(PyObject* const* a, Py_ssize_t n) {
+  Q8View c;
+  if (n != 9 || a[8] != Py_None || !q8_view(a[1], &c) || !on_current(*c.blocks)) return nullptr;
+  const at::Tensor *q = there(a[0], kBf16, *c.blocks), *lens = there(a[2], kI32, *c.blocks);
+  const at::Tensor *out = there(a[4], kBf16, *c.blocks), *parents;
+  if (!q || !lens || !out || q->dim() != 4 || !fits(*q) || out->sizes() != q->sizes()) return nullptr;
+  const int64_t N = q->size(1), H = q->size(2);
+  if (q->size(0) != c.B || q->size(3) != GLIDE_HEAD_DIM || !is_shape(*lens, {c.B}) ||
+      !optional_there(a[3], kI32, {c.B, N}, *c.blocks, &parents))
+    return nullptr;
+  float scale;
+  int splits;
+  if (!as_float(a[5], &scale) || !as_int(a[6], &splits)) return nullptr;
+  hipStream_t s;
+  at::Tensor ws;
+  if (a[7] == Py_None) {
+    PyObject* handle;
+    if (!stream_of(*q, &s, &handle)) return nullptr;
+    const size_t need = q8.attn_workspace(c.B, N, H, c.H, GLIDE_HEAD_DIM, c.cap, splits);
+    // under a capture the Python path finds the capture's own workspace
+    if (need == 0 || q8.capture_id(s)) {
+      Py_DECREF(handle);
+      if (need) return nullptr;
+    } else if (!kept_workspace(*q, handle, need, &ws)) {
+      return nullptr;
+    }
+  } else {
+    const at::Tensor* w = tensor(a[7]);
+    if (!w || w->device() != q->device() || !w->is_contiguous() || !stream_of(*q, &s, nullptr)) return nullptr;
+    ws = *w;
+  }
+  void* wp = ws.defined() ? ws.data_ptr() : nullptr;
+  const size_t ws_bytes = ws.defined() ? ws.numel() * ws.element_size() : 0;
+  void *qp = ptr(q), *op = ptr(out);
+  const int32_t *lp = (const int32_t*)ptr(lens), *pp = (const int32_t*)ptr(parents);
+  return status_of([&] {
+    return q8.attn(qp, &c.c, lp, pp, op, c.B, N, H, c.H, GLIDE_HEAD_DIM, c.cap, c.kind, scale, splits, wp, ws_bytes, s);
+  });
+}
+
+// (caches, seq_lens, accept_len, path, seq_lens_out, nodes, stream); the caches as a list
+PyObject* q8_commit(PyObject* const* a, Py_ssize_t n) {
+  if (n != 7 || a[6] != Py_None || !PyList_CheckExact(a[0])) return nullptr;
+  const Held caches(PyList_AsTuple(a[0]));  // the caches themselves are held, not the list
+  if (!caches.o) return nullptr;
+  const Py_ssize_t layers = PyTuple_GET_SIZE(caches.o);
+  if (layers < 1 || layers > 128) return nullptr;
+  Q8View first, v;
+  glide_q8_cache c[128];
+  for (Py_ssize_t i = 0; i < layers; ++i) {
+    Q8View* w = i ? &v : &first;
+    if (!q8_view(PyTuple_GET_ITEM(caches.o, i), w)) return nullptr;
+    if (i && (v.kind != first.kind || v.blocks->sizes() != first.blocks->sizes() ||
+              v.blocks->device() != first.blocks->device()))
+      return nullptr;
+    c[i] = w->c;
+  }
+  if (!on_current(*first.blocks)) return nullptr;
+  const int64_t B = first.B;
+  const at::Tensor *lens = there(a[1], kI32, *first.blocks), *acc = there(a[2], kI32, *first.blocks);
+  const at::Tensor *path = nullptr, *out = there(a[4], kI32, *first.blocks);
+  int N;
+  if (!lens || !acc || !out || !is_shape(*lens, {B}) || !is_shape(*acc, {B}) || !is_shape(*out, {B}) ||
+      !as_int(a[5], &N))
+    return nullptr;
+  if (a[3] != Py_None) {
+    path = there(a[3], kI32, *first.blocks);
+    if (!path || !is_shape(*path, {B, N})) return nullptr;
+  }
+  hipStream_t s;
+  if (!stream_of(*lens, &s, nullptr)) return nullptr;
+  const int32_t *lp = (const int32_t*)ptr(lens), *ap = (const int32_t*)ptr(acc), *pp = (const int32_t*)ptr(path);
+  int32_t* op = (int32_t*)ptr(out);
+  return status_of([&] {
+    return q8.commit(c, layers, lp, ap, pp, op, B, N, first.H, GLIDE_HEAD_DIM, first.cap, first.kind, s);
+  });
+}
+
 // The Python entry of a function above: nullptr and C++ exceptions (a tensor
 // without storage, an allocation that failed) become None.
 template <PyObject* (*F)(PyObject* const*, Py_ssize_t)>
@@ -339,6 +596,22 @@ PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t n) {
   Py_RETURN_NONE;
 }
 
+// bind_q8(addresses of the entry points in Q8Calls' order)
+PyObject* bind_q8(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  constexpr int kCalls = sizeof(Q8Calls) / sizeof(void*);
+  if (n != 1 || !PyTuple_Check(args[0]) || PyTuple_GET_SIZE(args[0]) != kCalls) {
+    PyErr_SetString(PyExc_TypeError, "bind_q8(addresses)");
+    return nullptr;
+  }
+  void* p[kCalls];
+  for (int i = 0; i < kCalls; ++i) {
+    p[i] = PyLong_AsVoidPtr(PyTuple_GET_ITEM(args[0], i));
+    if (PyErr_Occurred()) return nullptr;
+  }
+  memcpy(&q8, p, sizeof(q8));
+  Py_RETURN_NONE;
+}
+
 #define FAST(f) ((PyCFunction)(void (*)(void))(f))
 PyMethodDef methods[] = {{"bind", FAST(bind), METH_FASTCALL, nullptr},
                          {"tree_attn", FAST(entry<tree_attn>), METH_FASTCALL, nullptr},
@@ -347,6 +620,12 @@ PyMethodDef methods[] = {{"bind", FAST(bind), METH_FASTCALL, nullptr},
                          {"spec_sample", FAST(entry<spec_sample>), METH_FASTCALL, nullptr},
                          {"rows_matmul", FAST(entry<rows_matmul>), METH_FASTCALL, nullptr},
                          {"block_attn", FAST(entry<block_attn>), METH_FASTCALL, nullptr},
+                         {"bind_q8", FAST(bind_q8), METH_FASTCALL, nullptr},
+                         {"rope", FAST(entry<rope>), METH_FASTCALL, nullptr},
+                         {"q8_append", FAST(entry<q8_append>), METH_FASTCALL, nullptr},
+                         {"q8_read", FAST(entry<q8_read>), METH_FASTCALL, nullptr},
+                         {"q8_tree_attn", FAST(entry<q8_tree_attn>), METH_FASTCALL, nullptr},
+                         {"q8_commit", FAST(entry<q8_commit>), METH_FASTCALL, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

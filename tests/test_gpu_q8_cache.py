@@ -1,0 +1,372 @@
+"""The 8-bit cache on the GPU: written, read back and committed.
+
+Codes, scales and tail rows are compared exactly with the oracle (which divides
+in float32 as the definition says).  Read-back values are code * scale rounded
+once: off by at most eps / 2 of their size, plus 2^-24 of it for the float32
+product."""
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2402_02082_amd as glide
+from oracle import q8 as OQ
+from tests.gpu_common import cpu_normal, require_gpu, say
+
+pytestmark = pytest.mark.gpu
+
+BF, F32, I32 = torch.bfloat16, torch.float32, torch.int32
+KINDS = ["e4m3", "int8"]
+
+
+def ints(x):
+    return torch.tensor(x, dtype=I32, device="cuda")
+
+
+def f64(t):
+    return t.detach().double().cpu().numpy()
+
+
+def junk_cache(B, H, L_cap, kind, seed=0):
+    """A cache full of bytes that no call may take for a token: codes, scales and
+    tail rows that are not numbers."""
+    c = glide.q8_cache(B, H, L_cap, kind)
+    c.blocks.view(torch.uint8).fill_(0x7f)  # e4m3: NaN
+    c.scales.fill_(float("nan"))
+    c.tail.fill_(float("nan"))
+    return c
+
+
+def rows(shape, seed, spread=True):
+    """Rows whose channels and tokens differ in size."""
+    x = cpu_normal(shape, seed, F32)
+    if spread:
+        x = x * torch.exp(cpu_normal((1, 1, shape[2], 128), seed + 100, F32))
+        x = x * torch.exp(0.5 * cpu_normal((shape[0], shape[1], 1, 1), seed + 200, F32))
+    return x.to(BF).cuda()
+
+
+def check_cache(cache, k, v, lens, kind, held=None):
+    """The cache holds tokens k, v [b] [L, H, 128] exactly: whole blocks' codes
+    and scales, the tail's rows; held[b]: rows of a tree behind them."""
+    blocks, scales, tail = cache
+    values = blocks.float().cpu().numpy() - (128 if kind == "int8" else 0)
+    sc, tl = scales.cpu().numpy(), f64(tail)
+    H = blocks.shape[1]
+    for b, L in enumerate(lens):
+        for h in range(H):
+            for i in range(L // 32):
+                want = [OQ.quantise(f64(x[b][32 * i:32 * i + 32, h]), kind) for x in (k, v)]
+                assert np.array_equal(values[b, h, i], OQ.block_bytes(want[0][0], want[1][0])), (b, h, i)
+                assert sc[b, h, i].tolist() == [want[0][1], want[1][1]]
+        for m, x in ((0, k), (1, v)):
+            x = f64(x[b])
+            for j in range(L // 32 * 32, L):
+                assert np.array_equal(tl[b, :, m, j % 128], x[j]), (b, m, j)
+            if held is not None:
+                for t, row in enumerate(f64(held[m][b])):
+                    assert np.array_equal(tl[b, :, m, (L + t) % 128], row), (b, m, t)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("T", [1, 5, 31, 32, 33, 64, 100, 290])
+def test_append(kind, T):
+    """Ragged lengths, several appends in a row, junk everywhere else."""
+    require_gpu()
+    B, H, cap = 4, 3, 1024
+    cache = junk_cache(B, H, cap, kind)
+    all_k, all_v = rows((B, 700, H, 128), T), rows((B, 700, H, 128), T + 1)
+    lens = [0, 0, 0, 0]
+    counts = [1, 31, 32, 47]  # a ragged first append
+    glide.glide_q8_append(all_k[:, :47].contiguous(), all_v[:, :47].contiguous(), cache, ints(lens), ints(counts))
+    lens = counts
+    for step in range(2):
+        say("append", kind, T, lens)
+        k = torch.stack([all_k[b, n:n + T] for b, n in enumerate(lens)])
+        v = torch.stack([all_v[b, n:n + T] for b, n in enumerate(lens)])
+        glide.glide_q8_append(k, v, cache, ints(lens))
+        lens = [n + T for n in lens]
+        torch.cuda.synchronize()
+        check_cache(cache, all_k, all_v, lens, kind)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_append_one_by_one_equals_at_once(kind):
+    require_gpu()
+    B, H, n = 2, 2, 97
+    k, v = rows((B, n, H, 128), 3), rows((B, n, H, 128), 4)
+    one, all_ = junk_cache(B, H, 128, kind), junk_cache(B, H, 128, kind)
+    for t in range(n):
+        glide.glide_q8_append(k[:, t:t + 1].contiguous(), v[:, t:t + 1].contiguous(), one, ints([t, t]))
+    glide.glide_q8_append(k, v, all_, ints([0, 0]))
+    torch.cuda.synchronize()
+    assert torch.equal(one.blocks.view(torch.uint8), all_.blocks.view(torch.uint8))
+    assert torch.equal(one.scales[:, :, :3], all_.scales[:, :, :3])
+    assert torch.equal(one.tail[:, :, :, 96], all_.tail[:, :, :, 96])
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_append_writes_nothing_else(kind):
+    """Counts of 0, lengths clamped into the cache, rows past its end dropped;
+    bytes that hold no new token stay."""
+    require_gpu()
+    B, H, cap, T = 4, 2, 96, 40
+    k, v = rows((B, T, H, 128), 5), rows((B, T, H, 128), 6)
+    cache = junk_cache(B, H, cap, kind)
+    cache.scales.fill_(3.0)
+    cache.tail.fill_(5.0)
+    glide.glide_q8_append(k, v, cache, ints([10, 80, 500, -9]), ints([0, 40, 40, 99]))
+    torch.cuda.synchronize()
+    bytes_, scales, tail = cache.blocks.view(torch.uint8), cache.scales, cache.tail
+    changed = ((bytes_ != 0x7f).any(-1) | (scales != 3.0).any(-1)).all(1).tolist()
+    assert changed == [[False] * 3, [False, False, True], [False] * 3, [True, False, False]]
+    moved = (tail != 5.0).any(-1).any(2).all(1)
+    want = torch.zeros((B, 128), dtype=torch.bool)
+    want[3, 32:40] = True  # -9 counts as 0, 99 as 40; of 80 + 40 tokens 96 fit, and they fill blocks
+    assert torch.equal(moved.cpu(), want)
+
+
+@pytest.mark.parametrize("T", [1, 16, 63, 64])
+def test_hold(T):
+    """Tree rows go to the ring behind the accepted rows, and nowhere else."""
+    require_gpu()
+    B, H = 3, 2
+    lens = [31, 95, 1 << 20]  # the ring's end is passed
+    cache = glide.q8_cache(B, H, 1 << 20, "e4m3")
+    cache.blocks.view(torch.uint8).zero_()
+    cache.scales.fill_(3.0)
+    cache.tail.fill_(5.0)
+    k, v = rows((B, T, H, 128), 7), rows((B, T, H, 128), 8)
+    counts = [T, T, T - 1]
+    glide.glide_q8_append(k, v, cache, ints(lens), ints(counts), hold=True)
+    torch.cuda.synchronize()
+    assert not cache.blocks.view(torch.uint8).any() and bool((cache.scales == 3.0).all())
+    want = torch.full_like(cache.tail, 5.0)
+    for b in range(B):
+        for t in range(counts[b]):
+            want[b, :, 0, (lens[b] + t) % 128], want[b, :, 1, (lens[b] + t) % 128] = k[b, t], v[b, t]
+    assert torch.equal(cache.tail, want)
+
+
+@pytest.mark.parametrize("hold", [False, True])
+def test_append_takes_slices_of_a_projection(hold):
+    """Keys and values as slices of one [B, T, H, D] projection, and heads first."""
+    require_gpu()
+    B, T, H = 2, 50, 3
+    x = rows((B, T, 4 + 2 * H, 128), 9)
+    k, v = x[:, :, 4:4 + H], x[:, :, 4 + H:]
+    lens = ints([20, 0])
+    out = []
+    for a, b in ((k, v), (k.contiguous(), v.contiguous()),
+                 (k.transpose(1, 2).contiguous().transpose(1, 2), v.transpose(1, 2).contiguous().transpose(1, 2))):
+        c = junk_cache(B, H, 128, "int8")
+        c.tail.fill_(1.0)
+        glide.glide_q8_append(a, b, c, lens, hold=hold)
+        out.append(c)
+    torch.cuda.synchronize()
+    for c in out[1:]:
+        assert torch.equal(c.blocks, out[0].blocks) and torch.equal(c.tail, out[0].tail)
+        assert torch.equal(c.scales.view(I32), out[0].scales.view(I32))
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_quantisation_edges(kind):
+    """Blocks of zeros, of the type's largest and smallest values, of one value,
+    with signed zeros, and exact ties."""
+    require_gpu()
+    big = torch.finfo(BF).max
+    base = cpu_normal((32, 128), 10, F32)
+    ties = torch.arange(4096, dtype=F32).reshape(32, 128) % 256 / 256 * OQ.MOST[kind]
+    blocks = [torch.zeros(32, 128), -torch.zeros(32, 128), base * 1e-39, base * 1e-36, base.sign() * big,
+              torch.full((32, 128), -big), base * 0 + 1.0, ties, -ties, base.abs() * 2.0 ** -120]
+    blocks[0][3, 5] = torch.finfo(BF).tiny
+    blocks[6][31, 127] = 300.0
+    x = torch.stack(blocks).reshape(1, -1, 1, 128).to(BF).cuda()
+    cache = junk_cache(1, 1, x.shape[1], kind)
+    glide.glide_q8_append(x, x.flip(-1).contiguous(), cache, ints([0]))
+    torch.cuda.synchronize()
+    check_cache(cache, x, x.flip(-1), [x.shape[1]], kind)
+
+
+def test_not_finite_values_show():
+    """An infinity or NaN makes its block's scale one, and no other's."""
+    require_gpu()
+    x = rows((1, 96, 1, 128), 11)
+    x[0, 40, 0, 7], x[0, 70, 0, 100] = float("nan"), -float("inf")
+    for kind in KINDS:
+        cache = junk_cache(1, 1, 96, kind)
+        cache.scales.zero_()
+        glide.glide_q8_append(x, x, cache, ints([0]))
+        s = cache.scales[0, 0].cpu()
+        assert torch.isfinite(s[0]).all() and torch.isnan(s[1]).all() and torch.isinf(s[2]).all()
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "f32"])
+def test_read(kind, dtype):
+    require_gpu()
+    B, H, cap = 4, 2, 160
+    lens = [0, 31, 64, 150]
+    k, v = rows((B, 150, H, 128), 12), rows((B, 150, H, 128), 13)
+    cache = junk_cache(B, H, cap, kind)
+    glide.glide_q8_append(k, v, cache, ints([0] * B), ints(lens))
+    eps = torch.finfo(dtype).eps / 2 if dtype == BF else 2.0 ** -24
+    for start, T in ((0, 160), (0, 1), (33, 70), (64, 32), (149, 1), (130, 61)):
+        say("read", kind, str(dtype), start, T)
+        out = [torch.full((B, H, T, 128), 9.0, dtype=dtype, device="cuda") for _ in range(2)]
+        glide.glide_q8_read(cache, ints(lens), *out, start=start)
+        torch.cuda.synchronize()
+        for got, x in zip(out, (k, v)):
+            for b, L in enumerate(lens):
+                n = max(0, min(T, L - start))
+                assert bool((got[b, :, n:] == 9.0).all())  # rows behind the sequence stay
+                for h in range(H):
+                    want = OQ.stored(f64(x[b, :L, h]), kind)[start:start + n]
+                    err = np.abs(f64(got[b, h, :n]) - want)
+                    assert np.all(err <= (eps + 2.0 ** -24) * np.abs(want))
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("chain", [False, True])
+def test_commit_equals_appending_the_accepted_rows(kind, chain):
+    """Every layer's cache after a commit holds what appending the accepted
+    rows gives, whatever was held besides; lengths around block ends, none and
+    all 64 accepted."""
+    require_gpu()
+    H, N, layers = 2, 64, 3
+    rng = np.random.default_rng(14)
+    lens = [0, 1, 31, 32, 63, 64, 95, 127, 128, 200, 31, 30]
+    accept = [0, 1, 1, 64, 33, 32, 2, 64, 31, 5, 64, 40]
+    B = len(lens)
+    paths = [sorted(rng.choice(N, a, replace=False).tolist()) if not chain else list(range(a)) for a in accept]
+    path = None if chain else ints([p + [-1] * (N - len(p)) for p in paths])
+    got, want = [], []
+    for layer in range(layers):
+        k, v = rows((B, 200, H, 128), 20 + layer), rows((B, 200, H, 128), 30 + layer)
+        tk, tv = rows((B, N, H, 128), 40 + layer), rows((B, N, H, 128), 50 + layer)
+        pair = [junk_cache(B, H, 320, kind) for _ in range(2)]
+        for c in pair:
+            glide.glide_q8_append(k, v, c, ints([0] * B), ints(lens))
+        glide.glide_q8_append(tk, tv, pair[0], ints(lens), hold=True)
+        rk, rv = torch.zeros_like(tk), torch.zeros_like(tv)
+        for b, p in enumerate(paths):
+            rk[b, :len(p)], rv[b, :len(p)] = tk[b, p], tv[b, p]
+        glide.glide_q8_append(rk, rv, pair[1], ints(lens), ints(accept))
+        got.append(pair[0])
+        want.append(pair[1])
+    out = ints([-1] * B)
+    glide.glide_q8_commit(got, ints(lens), ints(accept), path, out)
+    torch.cuda.synchronize()
+    end = [a + b for a, b in zip(lens, accept)]
+    assert out.tolist() == end
+    for g, w in zip(got, want):
+        assert torch.equal(g.blocks.view(torch.uint8), w.blocks.view(torch.uint8))
+        assert torch.equal(g.scales.view(I32), w.scales.view(I32))
+        for b, n in enumerate(end):
+            for j in range(n // 32 * 32, n):
+                assert torch.equal(g.tail[b, :, :, j % 128], w.tail[b, :, :, j % 128]), (b, j)
+
+
+def test_commit_at_the_cache_end_and_out_of_range_data(monkeypatch):
+    require_gpu()
+    B, H = 4, 1
+    lens, accept = ints([60, 64, 63, 1000]), ints([9, 3, 1, -4])
+    cache = junk_cache(B, H, 64, "int8")
+    k = rows((B, 63, H, 128), 15)
+    glide.glide_q8_append(k, k, cache, ints([0] * B), ints([60, 63, 63, 63]))
+    t = rows((B, 12, H, 128), 16)
+    glide.glide_q8_append(t, t, cache, lens, hold=True)
+    out = ints([0] * B)
+    path = ints([[0, 1, 2, 99] + list(range(4, 12)), [5] * 12, [-7] * 12, [-1] * 12])
+    glide.glide_q8_commit([cache], lens, accept, path, out)
+    torch.cuda.synchronize()
+    assert out.tolist() == [64, 64, 64, 64]  # what fits; lengths clamped
+    want = [OQ.quantise(f64(torch.cat([k[0, 32:60], t[0, :4]])[:, 0]), "int8")[1],
+            OQ.quantise(f64(torch.cat([k[2, 32:63], t[2, :1]])[:, 0]), "int8")[1]]  # a bad node is the chain's
+    assert cache.scales[0, 0, 1].tolist() == [want[0]] * 2 and cache.scales[2, 0, 1].tolist() == [want[1]] * 2
+    monkeypatch.setenv("GLIDE_VALIDATE", "1")
+    ok_lens, ok_acc = ints([0, 1, 2, 63]), ints([0, 1, 2, 1])
+    ok_path = ints([[0, 1] + [-1] * 10] * B)
+
+    def commit(lens=ok_lens, acc=ok_acc, path=ok_path):
+        glide.glide_q8_commit([cache], lens, acc, path, out)
+
+    commit()
+    for kw in (dict(lens=lens), dict(acc=accept), dict(acc=ints([0, 1, 13, 1])), dict(acc=ints([0, 1, 2, 2])),
+               dict(path=ints([[1, 0] + [-1] * 10] * B)), dict(path=ints([[12, 13] + [-1] * 10] * B))):
+        with pytest.raises(glide.GlideError) as e:
+            commit(**kw)
+        assert e.value.status == glide.GLIDE_ERANGE
+    for fn in (lambda: glide.glide_q8_append(t, t, cache, ints([60] * B)),
+               lambda: glide.glide_q8_append(t, t, cache, ints([0] * B), ints([0, 1, 2, 13])),
+               lambda: glide.glide_q8_append(t, t, cache, ints([0, 0, 0, 65]), hold=True),
+               lambda: glide.glide_q8_read(cache, ints([0, 0, 0, -1]), k.transpose(1, 2).contiguous(),
+                                           k.transpose(1, 2).contiguous())):
+        with pytest.raises(glide.GlideError) as e:
+            fn()
+        assert e.value.status == glide.GLIDE_ERANGE
+    glide.glide_q8_append(t, t, cache, ints([64] * B), hold=True)
+
+
+def test_refusals():
+    require_gpu()
+    c = glide.q8_cache(2, 3, 64)
+    k, lens, out = torch.zeros((2, 4, 3, 128), dtype=BF, device="cuda"), ints([0, 0]), ints([0, 0])
+    wide = torch.zeros((2, 65, 3, 128), dtype=BF, device="cuda")
+    odd = torch.zeros((2, 4, 3, 132), dtype=BF, device="cuda")[..., 4:]
+    r = torch.zeros((2, 3, 64, 128), dtype=BF, device="cuda")
+    other = glide.q8_cache(2, 3, 64, "int8")
+    bad_caches = [list(c), c[:2], c._replace(blocks=c.blocks.view(torch.int8)), c._replace(blocks=c.blocks[..., :4096]),
+                  c._replace(scales=c.scales[:, :, :1]), c._replace(scales=c.scales.double()),
+                  c._replace(tail=c.tail.float()), c._replace(tail=c.tail[:, :, :1]), c._replace(tail=c.tail.cpu()),
+                  c._replace(blocks=c.blocks.transpose(0, 1))]
+    calls = [lambda x=x: glide.glide_q8_append(k, k, x, lens) for x in bad_caches]
+    calls += [lambda x=x: glide.glide_q8_read(x, lens, r, r) for x in bad_caches]
+    calls += [lambda x=x: glide.glide_q8_commit([x], lens, lens, None, out) for x in bad_caches]
+    calls += [
+        lambda: glide.glide_q8_append(k.float(), k.float(), c, lens), lambda: glide.glide_q8_append(k, k[:, :3], c, lens),
+        lambda: glide.glide_q8_append(k[:1], k[:1], c, lens), lambda: glide.glide_q8_append(k[:, :, :2], k[:, :, :2], c, lens),
+        lambda: glide.glide_q8_append(odd, odd, c, lens), lambda: glide.glide_q8_append(k[:, :0], k[:, :0], c, lens),
+        lambda: glide.glide_q8_append(k, odd, c, lens), lambda: glide.glide_q8_append(wide, wide, c, lens, hold=True),
+        lambda: glide.glide_q8_append(k, k, c, lens.long()), lambda: glide.glide_q8_append(k, k, c, lens[:1]),
+        lambda: glide.glide_q8_append(k, k, c, lens, lens[:1]), lambda: glide.glide_q8_append(k, k, c, lens.cpu()),
+        lambda: glide.glide_q8_read(c, lens, r, r.float()), lambda: glide.glide_q8_read(c, lens, r, r[:, :, :5]),
+        lambda: glide.glide_q8_read(c, lens, r.half(), r.half()), lambda: glide.glide_q8_read(c, lens, r, r, start=-1),
+        lambda: glide.glide_q8_read(c, lens, r, r, start=32), lambda: glide.glide_q8_read(c, lens, r[:1], r[:1]),
+        lambda: glide.glide_q8_commit([], lens, lens, None, out),
+        lambda: glide.glide_q8_commit([c, other], lens, lens, None, out),
+        lambda: glide.glide_q8_commit([c], lens, lens, None, lens),
+        lambda: glide.glide_q8_commit([c], lens, lens, lens, out),
+        lambda: glide.glide_q8_commit([c], lens, lens, torch.zeros((2, 65), dtype=I32, device="cuda"), out),
+        lambda: glide.glide_q8_commit([c], lens, lens, None, out, nodes=0),
+        lambda: glide.glide_q8_commit([c] * 129, lens, lens, None, out)]
+    for i, call in enumerate(calls):
+        with pytest.raises((ValueError, glide.GlideError)):
+            call()
+            pytest.fail("call %d was not refused" % i)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_offsets_past_32_bits(kind):
+    """A cache of 8 GiB: rows written, committed and read at its end."""
+    require_gpu()
+    H, cap = 8, 1 << 22
+    cache = glide.q8_cache(1, H, cap, kind)
+    L = cap - 70
+    k, v = rows((1, 100, H, 128), 17), rows((1, 100, H, 128), 18)
+    base = L // 32 * 32
+    # the tokens behind the last whole block, then some decoded ones, then a tree
+    glide.glide_q8_append(k[:, :L - base], v[:, :L - base], cache, ints([base]))
+    glide.glide_q8_append(k[:, L - base:60], v[:, L - base:60], cache, ints([L]))
+    n = base + 60
+    glide.glide_q8_append(k[:, 60:76], v[:, 60:76], cache, ints([n]), hold=True)
+    out = ints([0])
+    glide.glide_q8_commit([cache], ints([n]), ints([9]), None, out)
+    assert out.tolist() == [n + 9]
+    got = [torch.zeros((1, H, 69, 128), dtype=F32, device="cuda") for _ in range(2)]
+    glide.glide_q8_read(cache, out, *got, start=base)
+    torch.cuda.synchronize()
+    for g, x in zip(got, (k, v)):
+        for h in range(H):
+            want = OQ.stored(f64(x[0, :69, h]), kind)
+            assert np.all(np.abs(f64(g[0, h]) - want) <= 2.0 ** -23 * np.abs(want))
