@@ -639,8 +639,12 @@ int glide_q8_tree_attn(const void* q, const glide_q8_cache* cache, const int32_t
   a.seq_lens = seq_lens;
   a.parents = tree_parents;
   a.out = (uint16_t*)out;
-  a.part_o = p.ws_bytes ? (float*)((char*)workspace + p.part_o_off) : nullptr;
-  a.part_ml = p.ws_bytes ? (float2*)((char*)workspace + p.part_ml_off) : nullptr;
+  if (p.runs * p.groups > 2147483640L) return GLIDE_EINVAL;  // a grid dimension
+  if (p.ws_bytes > 0) {
+    a.counters = (unsigned*)workspace;
+    a.part_ml = (float2*)((char*)workspace + p.part_ml_off);
+    a.part_o = (float*)((char*)workspace + p.part_o_off);
+  }
   a.B = B;
   a.N = N;
   a.H = H;
@@ -648,9 +652,12 @@ int glide_q8_tree_attn(const void* q, const glide_q8_cache* cache, const int32_t
   a.n_blocks = L_cap / glide::kQ8Block;
   a.groups = p.groups;
   a.splits = p.splits;
+  a.target = p.target;
+  a.min_units = p.min_units;
+  a.runs = (int)p.runs;
   const double sc = scale > 0.f ? (double)scale : 1.0 / sqrt((double)D);
   a.scale_log2 = (float)(sc * 1.4426950408889634);  // log2(e)
-  return hip_status(glide::launch_q8_attn(a, kind == GLIDE_INT8, p.tiles, stream));
+  return hip_status(glide::launch_q8_attn(a, kind == GLIDE_INT8, p.rows, stream));
 }
 
 int glide_q8_commit(const glide_q8_cache* caches, int layers, const int32_t* seq_lens,

@@ -76,13 +76,15 @@ struct Q8CommitArgs {
 };
 hipError_t launch_q8_commit(const Q8CommitArgs& a, bool int8, hipStream_t stream);
 
-// How the attention over an 8-bit cache is divided: `tiles` 16-row query
-// tiles a workgroup, `groups` workgroups over the rows of a cached head,
-// `splits` over its keys.
+// How the attention over an 8-bit cache is divided: workgroups of `rows` query
+// rows, `groups` of them over the rows of a cached head, and its keys in runs of
+// units -- `splits` of every pair (sequence, cached head), or with splits == 0
+// about `target` of equal size in all, of at least min_units units each.  runs:
+// at most so many.
 struct Q8AttnPlan {
-  int tiles, groups, splits;
-  size_t ws_bytes;
-  size_t part_ml_off, part_o_off;
+  int rows, groups, splits, target, min_units;
+  long runs;
+  size_t ws_bytes, part_ml_off, part_o_off;
 };
 Q8AttnPlan plan_q8_attn(int B, int N, int H, int H_kv, int n_blocks, int max_splits);
 
@@ -92,12 +94,13 @@ struct Q8AttnArgs {
   const int32_t* seq_lens;
   const int32_t* parents;  // nullptr: cross mode
   uint16_t* out;
-  float* part_o;    // [B, H_kv, groups, splits, 16 tiles, D]: normalised outputs
-  float2* part_ml;  // [B, H_kv, groups, splits, 16 tiles]: (max in log2 units, sum)
-  int B, N, H, H_kv, n_blocks, groups, splits;
+  unsigned* counters;  // arrival counters of pairs that lie in several runs
+  float* part_o;    // [runs, groups, rows, D]: normalised outputs
+  float2* part_ml;  // [runs, groups, rows]: (max in log2 units, sum)
+  int B, N, H, H_kv, n_blocks, groups, splits, target, min_units, runs;
   float scale_log2;
 };
-hipError_t launch_q8_attn(const Q8AttnArgs& a, bool int8, int tiles, hipStream_t stream);
+hipError_t launch_q8_attn(const Q8AttnArgs& a, bool int8, int rows, hipStream_t stream);
 
 // Rotary positions of queries and keys.
 struct RopeRows {

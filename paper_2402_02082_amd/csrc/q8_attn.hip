@@ -5,12 +5,18 @@
 // for the tokens of whole blocks, and the ring's bfloat16 rows for those
 // behind them and for the tree.
 //
-// Work decomposition: the query rows of a cached head (N rows of each of the
-// H / H_kv query heads that share it) are cut into groups of up to 64, the
-// keys into units of 32 tokens -- the whole blocks, then the ring's rows --
-// and the units into splits.  One workgroup of four waves takes one split of
-// one group; its waves take units in turn, each for all of the group's rows,
-// so a byte of the cache is fetched and converted by one wave.
+// Work decomposition.  The query rows of a cached head (N rows of each of the
+// H / H_kv query heads that share it) are cut into groups of up to 64, its keys
+// into units of 32 tokens: the whole blocks, then the ring's rows.  Each pair
+// (sequence, cached head) is split into as many runs of units as its length
+// asks for, so that all runs of a call are of about the same size whatever the
+// sequences' lengths; a workgroup takes one run.  A pair of one run is finished
+// there; of the others each run leaves a state, counts itself in, and the one
+// that completes the pair joins the states in order, whichever that is: one
+// launch.
+// A workgroup's eight waves take units in turn, each for all of the group's rows
+// (up to 32 rows; 64 rows: four waves for each half, the second read of a unit
+// then comes from L2), so each code is converted by one or two waves.
 //
 // Per unit and wave, on v_mfma_f32_16x16x32:
 //   S^T[key, query] = K Q^T, softmax on S^T with one query per lane column,
@@ -44,7 +50,7 @@ typedef __attribute__((ext_vector_type(4))) float f32x4_t;
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4_t;
 
 constexpr int kD = kHeadDim;
-constexpr int kWaves = 4;
+constexpr int kWaves = 8;
 constexpr int kThreads = 64 * kWaves;
 
 __device__ __forceinline__ float neg_inf() { return -__builtin_huge_valf(); }
@@ -99,10 +105,30 @@ __device__ __forceinline__ u32x4_t decode8(uint32_t lo, uint32_t hi) {
   return r;
 }
 
-// Ancestor-or-self mask of node `lane` (bit m: node m), by pointer doubling;
-// parents outside [-1, lane) count as -1.  Called by a whole wave.
-__device__ __forceinline__ uint64_t ancestor_mask(const int32_t* parents, int N, int lane) {
-  int p = lane < N ? parents[lane] : -1;
+// The larger magnitude of each half, as bits (their order is that of the sizes).
+typedef __attribute__((ext_vector_type(2))) uint16_t u16x2_t;
+__device__ __forceinline__ uint32_t max_size(uint32_t top, uint32_t bf16s) {
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2_t, top),
+                                                                __builtin_bit_cast(u16x2_t, bf16s & 0x7fff7fffu)));
+}
+__device__ __forceinline__ uint32_t larger_half(uint32_t v) { return max(v & 0xffffu, v >> 16); }
+
+// Maximum over a wave: within the 16-lane rows (neighbours, pairs, half mirror,
+// mirror), then across them.
+template <int CTRL>
+__device__ __forceinline__ uint32_t max_moved(uint32_t v) {
+  return max(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, CTRL, 0xF, 0xF, true));
+}
+__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
+  v = max_moved<0x140>(max_moved<0x141>(max_moved<0x4E>(max_moved<0xB1>(v))));
+  return max(max(__builtin_amdgcn_readlane(v, 0), __builtin_amdgcn_readlane(v, 16)),
+             max(__builtin_amdgcn_readlane(v, 32), __builtin_amdgcn_readlane(v, 48)));
+}
+
+// Ancestor-or-self mask of node `lane` (bit m: node m) from its parent, by
+// pointer doubling; parents outside [-1, lane) count as -1.  Called by a whole
+// wave.
+__device__ __forceinline__ uint64_t ancestor_mask(int p, int lane) {
   if (p < -1 || p >= lane) p = -1;
   uint32_t lo = lane < 32 ? 1u << lane : 0u, hi = lane < 32 ? 0u : 1u << (lane - 32);
   for (int round = 0; round < 6 && __any(p >= 0); ++round) {
@@ -114,48 +140,57 @@ __device__ __forceinline__ uint64_t ancestor_mask(const int32_t* parents, int N,
   return ((uint64_t)hi << 32) | lo;
 }
 
-constexpr float kRescaleSlack = 8.f;     // log2: how far a score may pass the reference maximum
-constexpr float kProductTop = 32768.f;   // a product p * s * c at which c moves
-constexpr float kProductAim = 128.f;     // and where the largest is put
-constexpr float kFactorMost = 8.507e37f;  // c at most 2^126
+constexpr int kRingCost = 4;  // blocks that take a wave about as long as a unit of ring rows
+
+constexpr float kRescaleSlack = 8.f;  // how far a score may pass the reference maximum (log2)
+constexpr float kProductTop = 15.f;   // log2 of a product p * s * c at which c moves,
+constexpr float kProductAim = 7.f;    // and of where the largest is put
+constexpr float kFactorMost = 126.f;  // log2 of c at most
+constexpr float kNoFactor = 1e30f;
 
 // State of one query row (lane column) over the keys that its wave has seen.
 struct RowState {
-  float m;  // reference maximum of the scaled scores (log2 units); -inf: none
-  float l;  // sum of 2^(score - m) over this lane's keys
-  float c;  // accumulators are sums of 2^(score - m) * c * value; 0: none but zeros yet
+  float m;   // reference maximum of the scaled scores (log2 units); -inf: none
+  float l;   // sum of 2^(score - m) over this lane's keys
+  float c;   // accumulators are sums of 2^(score - m) * c * value; 0: none but zeros yet
+  float lc;  // log2 of c; kNoFactor: c is 0
 };
 
-// Turns the scores x[8] of a unit (masked ones -inf) into 2^(x - m), moving m
-// and c where needed; s is the size of the unit's values (a code counts as 1).
-__device__ __forceinline__ void softmax_unit(float (&x)[8], RowState& st, f32x4_t (&acc)[8], float s) {
-  float mx = x[0];
-#pragma unroll
-  for (int i = 1; i < 8; ++i) mx = __builtin_elementwise_maximum(mx, x[i]);
+// Turns the raw scores x[8] of a unit (masked ones -inf), to be multiplied by
+// k >= 0, into 2^(x k - m), moving m and c where needed; ls is log2 of the
+// size of the unit's values (a code counts as 1).
+__device__ __forceinline__ void softmax_unit(float (&x)[8], RowState& st, f32x4_t (&acc)[8], float k, float ls) {
+  float mx = __builtin_elementwise_maximum(
+      __builtin_elementwise_maximum(__builtin_elementwise_maximum(x[0], x[1]), x[2]),
+      __builtin_elementwise_maximum(__builtin_elementwise_maximum(__builtin_elementwise_maximum(x[3], x[4]), x[5]),
+                                    __builtin_elementwise_maximum(x[6], x[7])));
+  mx *= k;
   if (__any(mx > st.m + kRescaleSlack)) {
     const float m_new = fmaxf(st.m, max_across_groups(mx));
     if (st.m != neg_inf()) {
       st.l *= fast_exp2(st.m - m_new);
-      st.c = fminf(st.c * fast_exp2(m_new - st.m), kFactorMost);
+      if (st.lc != kNoFactor) {
+        st.lc = fminf(st.lc + (m_new - st.m), kFactorMost);
+        st.c = fast_exp2(st.lc);
+      }
     }
     st.m = m_new;
   }
   const float m_ref = st.m == neg_inf() ? 0.f : st.m;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) x[i] = fast_exp2(x[i] - m_ref);
-  st.l += ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
-  const float f = s * st.c;
-  const float top = fast_exp2(mx - m_ref);
-  if (__any(top * f > kProductTop || (st.c == 0.f && top > 0.f && s > 0.f))) {
-    const float col = max_across_groups(top);
-    if (col * f > kProductTop || (st.c == 0.f && col > 0.f && s > 0.f)) {
-      const float c = fminf(kProductAim / col / s, kFactorMost);
-      const float r = st.c > 0.f ? c / st.c : 0.f;
+  if (__any((mx - m_ref) + (ls + st.lc) > kProductTop)) {
+    const float col = max_across_groups(mx) - m_ref;
+    if (col + (ls + st.lc) > kProductTop) {
+      const float lc = fminf(kProductAim - col - ls, kFactorMost);
+      const float r = st.lc == kNoFactor ? 0.f : fast_exp2(lc - st.lc);
 #pragma unroll
       for (int t = 0; t < 8; ++t) acc[t] *= r;
-      st.c = c;
+      st.lc = lc;
+      st.c = fast_exp2(lc);
     }
   }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = fast_exp2(fmaf(x[i], k, -m_ref));
+  st.l += ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
 }
 
 // Infinities and NaN of a unit's values reach only the rows that see them:
@@ -188,119 +223,331 @@ __device__ __forceinline__ f32x4_t add_not_finite(u32x4_t& w, uint32_t seen) {
   return add;
 }
 
-template <int NT, bool INT8, bool TREE>
+// A block's codes as they lie in memory: four 1 KB loads of K, four of V.
+struct RawUnit {
+  u32x4_t k[4], v[4];
+};
+
+// Buffer descriptor of one block, empty where the unit is past the last: such
+// loads return zeros without touching memory, so the pipeline needs no guard.
+constexpr int kBufferDesc3 = 0x00020000;  // 32-bit data, raw addressing
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t unit_rsrc(const uint8_t* blocks, int u, int u_end) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(blocks) + (size_t)u * kQ8BlockBytes, (short)0,
+                                           u < u_end ? kQ8BlockBytes : 0, kBufferDesc3);
+}
+// Cache policy of these loads: non-temporal where every byte is read once.
+constexpr int kKeep = 0, kStream = 2;
+template <int CPOL>
+__device__ __forceinline__ void load_k(RawUnit& f, __amdgpu_buffer_rsrc_t r, int lane) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    f.k[i] = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(r, lane * 16 + 1024 * i, 0, CPOL));
+}
+template <int CPOL>
+__device__ __forceinline__ void load_v(RawUnit& f, __amdgpu_buffer_rsrc_t r, int lane) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    f.v[i] = __builtin_bit_cast(
+        u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(r, lane * 16 + kQ8PartBytes + 1024 * i, 0, CPOL));
+}
+
+// Tokens and units of sequence b.  A sequence without keys counts as one unit,
+// so that some workgroup writes its zeros.
+struct Seq {
+  int L, end, units;
+};
+__device__ __forceinline__ Seq sequence(const Q8AttnArgs& a, bool tree, int b) {
+  Seq s;
+  s.L = min(max(a.seq_lens[b], 0), a.n_blocks * kQ8Block);
+  s.end = s.L + (tree ? a.N : 0);
+  s.units = max(1, (s.end + kQ8Block - 1) / kQ8Block);
+  return s;
+}
+
+// Inclusive sum over a wave, by moves inside and across its 16-lane rows.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int add_moved(int v) {
+  return v + __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xF, false);
+}
+__device__ __forceinline__ int scan64(int v) {
+  v = add_moved<0x111, 0xF>(v);  // one, two, four, eight lanes up
+  v = add_moved<0x112, 0xF>(v);
+  v = add_moved<0x114, 0xF>(v);
+  v = add_moved<0x118, 0xF>(v);
+  v = add_moved<0x142, 0xA>(v);  // row 0's and 2's last lane to the row behind
+  return add_moved<0x143, 0xC>(v);  // lane 31 to the upper half
+}
+
+// The run of a workgroup: units [u0, u1) of (b, hk), the first of `n` runs of
+// that pair being number `first` and the others a.H_kv apart.
+struct Run {
+  int b, hk, u0, u1, n, first;
+};
+
+// Runs of a sequence of so many units.
+__device__ __forceinline__ int runs_of(const Q8AttnArgs& a, int units, int per) {
+  return a.splits ? a.splits : (units + per - 1) / per;
+}
+
+// Run number `run`; false past the last.  Called by whole waves; sequences are
+// looked through 64 at a time, one a lane.
+__device__ __forceinline__ bool find_run(const Q8AttnArgs& a, bool tree, int run, int lane, Run* r) {
+  int b = 0, before = 0, per = 1;
+  if (a.splits) {
+    b = run / (a.splits * a.H_kv);
+    if (b >= a.B) return false;
+    before = b * a.splits * a.H_kv;
+    if (a.splits == 1 && a.B >= 2 && a.B <= 64) {
+      // the b-th longest sequence (of equals the first): the longest start first,
+      // and the shorter ones fill in as CUs come free
+      const int len = lane < a.B ? a.seq_lens[lane] : 0;
+      int rank = 0;
+      for (int j = 0; j < a.B; ++j) {
+        const int lj = __builtin_amdgcn_readlane(len, j);
+        rank += lj > len || (lj == len && j < lane);
+      }
+      b = __ffsll((long long)__ballot(lane < a.B && rank == b)) - 1;
+    }
+  } else if (a.B == 1) {
+    const int units = sequence(a, tree, 0).units;
+    per = max((units * a.H_kv + a.target - 1) / a.target, a.min_units);
+  } else {
+    int total = 0;
+    for (int b0 = 0; b0 < a.B; b0 += 64) total += b0 + lane < a.B ? sequence(a, tree, b0 + lane).units : 0;
+    total = __builtin_amdgcn_readlane(scan64(total), 63);
+    per = max((total * a.H_kv + a.target - 1) / a.target, a.min_units);
+    int sum = 0;
+    bool found = false;
+    for (int b0 = 0; b0 < a.B && !found; b0 += 64) {
+      const int n = b0 + lane < a.B ? runs_of(a, sequence(a, tree, b0 + lane).units, per) * a.H_kv : 0;
+      const int incl = sum + scan64(n);
+      const uint64_t hit = __ballot(run < incl);
+      found = hit != 0;
+      const int l = found ? __ffsll((long long)hit) - 1 : 63;
+      b = b0 + l;
+      before = __builtin_amdgcn_readlane(incl - n, l);
+      sum = __builtin_amdgcn_readlane(incl, 63);
+    }
+    if (!found) return false;
+  }
+  b = __builtin_amdgcn_readfirstlane(b);
+  const int units = __builtin_amdgcn_readfirstlane(sequence(a, tree, b).units);
+  const int n = runs_of(a, units, per), rest = run - before, i = rest / a.H_kv;
+  if (i >= n) return false;  // (a single sequence: past its last run)
+  const int size = (units + n - 1) / n;
+  r->b = b, r->hk = rest - i * a.H_kv, r->n = n, r->first = before + r->hk;
+  r->u0 = min(units, i * size), r->u1 = min(units, r->u0 + size);
+  return true;
+}
+
+// States are written and read with the device-scope cache policy (sc1), so that
+// the joining workgroup sees them whichever XCD wrote them.
+constexpr int kDeviceScope = 16;
+typedef __attribute__((ext_vector_type(2))) uint32_t u32x2_t;
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t state_rsrc(void* p, int bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(p, (short)0, bytes, kBufferDesc3);
+}
+
+// Counts a run's state in once its stores have completed at device scope;
+// true in the workgroup that completes the pair (which resets the counter).
+__device__ __forceinline__ bool last_to_arrive(unsigned* counter, int n, int* flag) {
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    const unsigned before = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    const bool last = before == (unsigned)(n - 1);
+    if (last) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    *flag = last;
+  }
+  __syncthreads();
+  return *flag != 0;
+}
+
+constexpr int kPitch = kD + 4;  // floats between LDS rows, so that rows start in other banks
+template <int ROWS>  // query rows of a wave
+struct JoinLds {
+  float m[kWaves][ROWS], l[kWaves][ROWS];
+  __attribute__((aligned(16))) float o[kWaves][ROWS][kPitch];
+  int flag;
+};
+
+// 1 / sum of a row's probabilities; 0 where it saw no key, and NaN stays.
+__device__ __forceinline__ float reciprocal(float l) { return l > 0.f ? __builtin_amdgcn_rcpf(l) : (l == 0.f ? 0.f : l); }
+
+// Maximum and sum of a row over a group's key waves.
+template <int WAVES, class Lds>
+__device__ __forceinline__ void join_sums(const Lds& lds, int first, int row, float& M, float& L) {
+  float m[WAVES], l[WAVES];
+#pragma unroll
+  for (int w = 0; w < WAVES; ++w) m[w] = lds.m[first + w][row], l[w] = lds.l[first + w][row];
+  M = m[0];
+#pragma unroll
+  for (int w = 1; w < WAVES; ++w) M = fmaxf(M, m[w]);
+  const float ref = M == neg_inf() ? 0.f : M;
+  L = 0.f;
+#pragma unroll
+  for (int w = 0; w < WAVES; ++w) L += fast_exp2(m[w] - ref) * l[w];
+}
+
+// The states of a pair joined in run order into output rows.  State i of n is in
+// the slot of its run, first + i * H_kv; `rows` of the group's kRows are in use.  16 lanes take a row, so a wave takes four at a time; where
+// the rows do not fill the waves, several waves share a row's states.
+template <int kRows, class Lds>
+__device__ __forceinline__ void join_states(const Q8AttnArgs& a, int first, int n, int grp, int rows, uint16_t* out,
+                                            int row_first, int G, Lds& lds) {
+  constexpr int kBatch = 8;  // states requested at once
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int quads = (rows + 3) / 4;
+  const int parts = quads == 1 ? 8 : (quads == 2 ? 4 : (quads <= 4 ? 2 : 1));  // waves that share a row
+  const int part = wave % parts, d = lane % 16 * 8;
+  for (int quad = wave / parts; quad < quads; quad += kWaves / parts) {
+    const int row = 4 * quad + lane / 16;
+    const bool live = row < rows;
+    float M = neg_inf(), L = 0.f, o[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) o[e] = 0.f;
+    for (int s0 = part; s0 < n; s0 += kBatch * parts) {
+      f32x2_t ml[kBatch];
+      f32x4_t x[kBatch][2];
+#pragma unroll
+      for (int j = 0; j < kBatch; ++j) {
+        const int i = min(s0 + j * parts, n - 1);
+        const size_t at = ((size_t)(first + i * a.H_kv) * a.groups + grp) * kRows;
+        const __amdgpu_buffer_rsrc_t rm = state_rsrc(a.part_ml + at, rows * 8);
+        const __amdgpu_buffer_rsrc_t ro = state_rsrc(a.part_o + at * kD, rows * kD * 4);
+        ml[j] = __builtin_bit_cast(f32x2_t, __builtin_amdgcn_raw_buffer_load_b64(rm, row * 8, 0, kDeviceScope));
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+          x[j][h] = __builtin_bit_cast(
+              f32x4_t, __builtin_amdgcn_raw_buffer_load_b128(ro, (row * kD + d + 4 * h) * 4, 0, kDeviceScope));
+      }
+#pragma unroll
+      for (int j = 0; j < kBatch; ++j) {
+        if (s0 + j * parts >= n || ml[j][1] == 0.f) continue;  // a run that saw no key
+        const float m = fmaxf(M, ml[j][0]);
+        const float ref = m == neg_inf() ? 0.f : m;
+        const float keep = fast_exp2(M - ref), w = fast_exp2(ml[j][0] - ref) * ml[j][1];
+        L = L * keep + w;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[e] = o[e] * keep + w * x[j][e >> 2][e & 3];
+        M = m;
+      }
+    }
+    if (parts > 1) {  // up to 16 rows, and one turn of this loop
+      const int slot = row;
+      lds.m[part][slot] = M, lds.l[part][slot] = L;
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        *(f32x4_t*)&lds.o[part][slot][d + 4 * h] = f32x4_t{o[4 * h], o[4 * h + 1], o[4 * h + 2], o[4 * h + 3]};
+      __syncthreads();
+      M = neg_inf(), L = 0.f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) o[e] = 0.f;
+      for (int p = 0; p < parts; ++p) M = fmaxf(M, lds.m[p][slot]);
+      for (int p = 0; p < parts; ++p) {
+        if (lds.l[p][slot] == 0.f) continue;
+        const float w = fast_exp2(lds.m[p][slot] - (M == neg_inf() ? 0.f : M));
+        L += w * lds.l[p][slot];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[e] += w * lds.o[p][slot][d + e];
+      }
+    }
+    if (live && part == 0) {
+      const float inv = reciprocal(L);
+      const int r = row_first + row, node = r / G;
+      u32x4_t w;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) w[e] = pack_bf16x2(o[2 * e] * inv, o[2 * e + 1] * inv);
+      *(u32x4_t*)(out + ((size_t)node * a.H + (r - node * G)) * kD + d) = w;
+    }
+  }
+}
+
+template <int NT, int RG, bool INT8, bool TREE>
 __global__ __launch_bounds__(kThreads) void q8_attn_kernel(Q8AttnArgs a) {
-  const int hk = blockIdx.x % a.H_kv, grp = blockIdx.x / a.H_kv, b = blockIdx.y, split = blockIdx.z;
+  constexpr int kKeyWaves = kWaves / RG;
+  constexpr int kStages = NT == 1 ? 2 : 1;
+  constexpr int kPolicy = RG == 1 ? kStream : kKeep;
+  constexpr int kRows = 16 * NT * RG;  // query rows of a workgroup
   const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int G = a.H / a.H_kv, R = a.N * G, row0 = grp * 16 * NT;
-  const int cap = a.n_blocks * kQ8Block;
-  const int L = __builtin_amdgcn_readfirstlane(min(max(a.seq_lens[b], 0), cap));
-  const int end = L + (TREE ? a.N : 0);
-  const int whole = L / kQ8Block, units = (end + kQ8Block - 1) / kQ8Block;
-  const int per = (units + a.splits - 1) / a.splits;
-  const int u0 = split * per, u1 = min(units, u0 + per);
+  const int kw = wave % kKeyWaves, rg = wave / kKeyWaves;
+  // Workgroups go to the eight XCDs in turn; the groups of a run are eight
+  // apart, on the same XCD and so on the same L2, which they share its keys in.
+  const int grp = a.groups == 1 ? 0 : blockIdx.x / 8 % a.groups;
+  const int run = a.groups == 1 ? blockIdx.x : blockIdx.x / (8 * a.groups) * 8 + blockIdx.x % 8;
+  const int G = a.H / a.H_kv, R = a.N * G, row0 = grp * kRows + rg * 16 * NT;
+  __shared__ JoinLds<16 * NT> lds;
 
+  Run rn;
+  if (!find_run(a, TREE, run, lane, &rn)) return;
+  const int b = rn.b, hk = rn.hk, u0 = rn.u0, u1 = rn.u1;
+  const Seq seq = sequence(a, TREE, b);
+  const int L = __builtin_amdgcn_readfirstlane(seq.L), end = __builtin_amdgcn_readfirstlane(seq.end);
+  const int whole = L / kQ8Block;
   const size_t head = (size_t)b * a.H_kv + hk;
   const uint8_t* blocks = a.cache.blocks + head * a.n_blocks * (size_t)kQ8BlockBytes;
   const float* scales = a.cache.scales + head * a.n_blocks * 2;
 
-  // Query rows: row r is node r / G of query head hk * G + r % G.
-  const uint16_t* qrow[NT];
-  bool live[NT];
+  // The run's units among its key waves.  The last waves take one ring unit each
+  // (a ring holds at most 95 rows, three units); the blocks go in turn, but that
+  // waves without a ring unit take kRingCost of them before.
+  static_assert(kKeyWaves > 3, "a ring unit a wave");
+  const int ue = min(u1, whole), ring_units = max(0, u1 - max(u0, whole));
+  const bool ring = kw >= kKeyWaves - ring_units;
+  const int early_waves = ring_units ? kKeyWaves - ring_units : 0, turns = u0 + early_waves * kRingCost;
+  int u = early_waves && !ring ? u0 + kw : turns + kw;
+  auto next = [&](int at) {
+    const int more = at + early_waves;
+    return at >= turns ? at + kKeyWaves : (more < turns ? more : turns + kw);
+  };
+  RawUnit raw[kStages];
+  float2 unit_scale[kStages];  // of K, of V
+  auto load_scale = [&](int at) { return *(const float2*)(scales + 2 * min(at, a.n_blocks - 1)); };
+  auto prefetch = [&] {
+#pragma unroll
+    for (int i = 0; i < kStages; ++i) {
+      const int at = i ? next(u) : u;
+      unit_scale[i] = load_scale(at);
+      const __amdgpu_buffer_rsrc_t r = unit_rsrc(blocks, at, ue);
+      load_k<kPolicy>(raw[i], r, lane);
+      load_v<kPolicy>(raw[i], r, lane);
+    }
+  };
+  // Query rows: row r is node r / G of query head hk * G + r % G.  MFMA step
+  // 2 h + e holds dims 64 h + 16 g + 8 e + (0..7).
   int node[NT];
-  u32x4_t qf[NT][4];   // MFMA step 2 h + e: dims 64 h + 16 g + 8 e + (0..7)
-  float qscale[NT];
+  u32x4_t qf[NT][4];
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
     const int r = row0 + 16 * nt + c;
-    live[nt] = r < R;
-    node[nt] = live[nt] ? r / G : 0;
-    qrow[nt] = a.q + (((size_t)b * a.N + node[nt]) * a.H + hk * G + (live[nt] ? r % G : 0)) * kD;
-    u32x4_t raw[4];
-    uint32_t top = 0;
-#pragma unroll
-    for (int st = 0; st < 4; ++st) {
-      raw[st] = live[nt] ? *(const u32x4_t*)(qrow[nt] + 64 * (st >> 1) + 16 * g + 8 * (st & 1)) : u32x4_t{0, 0, 0, 0};
-#pragma unroll
-      for (int e = 0; e < 4; ++e) top = max(top, max(raw[st][e] & 0x7fffu, (raw[st][e] >> 16) & 0x7fffu));
-    }
-    const float col = max_across_groups(__uint_as_float(min(top, 0x7f7fu) << 16));
-    const int ex = max((int)(__float_as_uint(col) >> 23), 15);  // biased exponent; q * 2^(141 - ex) is below 2^15
-    const float up = __uint_as_float((uint32_t)(268 - ex) << 23);
-    qscale[nt] = a.scale_log2 * __uint_as_float((uint32_t)(ex - 14) << 23);
+    node[nt] = r < R ? r / G : 0;
+    const uint16_t* q = a.q + (((size_t)b * a.N + node[nt]) * a.H + hk * G + (r - node[nt] * G)) * kD;
 #pragma unroll
     for (int st = 0; st < 4; ++st)
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        qf[nt][st][e] = pack_f16x2(__uint_as_float(raw[st][e] << 16) * up, __uint_as_float(raw[st][e] & 0xffff0000u) * up);
+      qf[nt][st] = r < R ? *(const u32x4_t*)(q + 64 * (st >> 1) + 16 * g + 8 * (st & 1)) : u32x4_t{0, 0, 0, 0};
   }
+
+  // The first blocks are requested now, unless the wave has ring rows and no
+  // registers to hold the blocks through their scores.
+  const bool later = kStages == 1 && ring;
+  if (!later) prefetch();
 
   RowState sm[NT];
   f32x4_t acc[NT][8];
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
-    sm[nt] = RowState{neg_inf(), 0.f, 0.f};
+    sm[nt] = RowState{neg_inf(), 0.f, 0.f, kNoFactor};
 #pragma unroll
     for (int t = 0; t < 8; ++t) acc[nt][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   }
 
-  int u = u0 + wave;
-  for (; u < min(u1, whole); u += kWaves) {
-    const uint8_t* p = blocks + (size_t)u * kQ8BlockBytes + lane * 16;
-    const float ks = scales[2 * u], vs = scales[2 * u + 1];
-    u32x4_t kraw[4], vraw[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) kraw[i] = *(const u32x4_t*)(p + 1024 * i);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) vraw[i] = *(const u32x4_t*)(p + kQ8PartBytes + 1024 * i);
-    f32x4_t s[2][NT];
-#pragma unroll
-    for (int kt = 0; kt < 2; ++kt) {
-      u32x4_t kf[4];
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const u32x4_t w = kraw[2 * kt + h];
-        kf[2 * h] = decode8<INT8>(w[0], w[1]);
-        kf[2 * h + 1] = decode8<INT8>(w[2], w[3]);
-      }
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        f32x4_t x = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int st = 0; st < 4; ++st)
-          x = __builtin_amdgcn_mfma_f32_16x16x32_f16(as_f16x8(kf[st]), as_f16x8(qf[nt][st]), x, 0, 0, 0);
-        s[kt][nt] = x;
-      }
-    }
-    u32x4_t vf[8];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      vf[2 * i] = decode8<INT8>(vraw[i][0], vraw[i][1]);
-      vf[2 * i + 1] = decode8<INT8>(vraw[i][2], vraw[i][3]);
-    }
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      const float k = qscale[nt] * ks;
-      float x[8];
-#pragma unroll
-      for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) x[4 * kt + r] = s[kt][nt][r] * k;
-      softmax_unit(x, sm[nt], acc[nt], vs);
-      const float f = vs * sm[nt].c;
-      u32x4_t pf;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) pf[e] = pack_f16x2(x[2 * e] * f, x[2 * e + 1] * f);
-#pragma unroll
-      for (int t = 0; t < 8; ++t)
-        acc[nt][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(as_f16x8(vf[t]), as_f16x8(pf), acc[nt][t], 0, 0, 0);
-    }
-  }
-
-  // At most one unit of ring rows a wave (a ring holds at most 95 rows).
-  if (u < u1) {
-    const int j0 = u * kQ8Block;
+  // Ring rows, taken first.
+  if (ring) {
+    const int j0 = (max(u0, whole) + kKeyWaves - 1 - kw) * kQ8Block;
+    int parent = -1;
+    if (TREE && lane < a.N) parent = a.parents[(size_t)b * a.N + lane];
     const uint16_t* kt_rows = a.cache.tail + head * kQ8TailElems + (j0 & (kQ8Tail - 1)) * kD;
     const uint16_t* vt_rows = kt_rows + kQ8Tail * kD;
     u32x4_t kf[2][4], v[8];
@@ -309,26 +556,31 @@ __global__ __launch_bounds__(kThreads) void q8_attn_kernel(Q8AttnArgs a) {
 #pragma unroll
       for (int st = 0; st < 4; ++st)
         kf[kt][st] = *(const u32x4_t*)(kt_rows + (16 * kt + c) * kD + 64 * (st >> 1) + 16 * g + 8 * (st & 1));
-    bool odd = false;  // a value that is not finite
-    uint32_t top = 0;
+    uint32_t top = 0;  // the largest size of the unit's values
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const int row = 16 * (i >> 2) + 4 * g + (i & 3);
       v[i] = *(const u32x4_t*)(vt_rows + row * kD + 8 * c);
       if (j0 + row >= end) v[i] = u32x4_t{0, 0, 0, 0};  // rows that hold no token
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const uint32_t lo = v[i][e] & 0x7fffu, hi = (v[i][e] >> 16) & 0x7fffu;
-        odd |= max(lo, hi) >= 0x7f80u;
-        top = max(top, max(lo < 0x7f80u ? lo : 0u, hi < 0x7f80u ? hi : 0u));
-      }
+      for (int e = 0; e < 4; ++e) top = max_size(top, v[i][e]);
     }
-    odd = __any(odd);
+    top = larger_half(top);
+    const bool odd = __any(top >= 0x7f80u);  // an infinity or NaN among them
+    if (odd) {
+      top = 0;
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, d));
-    const float size = __uint_as_float(top << 16) * (1.f / 256);  // as if the largest value were a code of 256
+      for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t lo = v[i][e] & 0x7fffu, hi = (v[i][e] >> 16) & 0x7fffu;
+          top = max(top, max(lo < 0x7f80u ? lo : 0u, hi < 0x7f80u ? hi : 0u));
+        }
+    }
+    top = wave_max(top);
+    const float ls = __builtin_amdgcn_logf(__uint_as_float(top << 16)) - 8.f;  // as if the largest were a code of 256
     uint64_t mine = 0;  // ancestor mask of node `lane`
-    if (TREE) mine = ancestor_mask(a.parents + (size_t)b * a.N, a.N, lane);
+    if (TREE) mine = ancestor_mask(parent, lane);
     u32x4_t vt[8];  // V^T operands: tile t holds dim 8 c + t of the lane's eight tokens
 #pragma unroll
     for (int w = 0; w < 4; ++w)
@@ -337,37 +589,39 @@ __global__ __launch_bounds__(kThreads) void q8_attn_kernel(Q8AttnArgs a) {
         vt[2 * w][e] = __builtin_amdgcn_perm(v[2 * e + 1][w], v[2 * e][w], 0x05040100u);
         vt[2 * w + 1][e] = __builtin_amdgcn_perm(v[2 * e + 1][w], v[2 * e][w], 0x07060302u);
       }
+    f32x4_t s[2][NT];
+#pragma unroll
+    for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        f32x4_t x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int st = 0; st < 4; ++st)
+          x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(kf[kt][st]), as_bf16x8(qf[nt][st]), x, 0, 0, 0);
+        s[kt][nt] = x;
+      }
+    if (later) prefetch();
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-      u32x4_t qb[4];
-#pragma unroll
-      for (int st = 0; st < 4; ++st)
-        qb[st] = live[nt] ? *(const u32x4_t*)(qrow[nt] + 64 * (st >> 1) + 16 * g + 8 * (st & 1)) : u32x4_t{0, 0, 0, 0};
       uint64_t anc = 0;
       if (TREE)
         anc = ((uint64_t)(uint32_t)__shfl((uint32_t)(mine >> 32), node[nt]) << 32) | (uint32_t)__shfl((uint32_t)mine, node[nt]);
       float x[8];
       uint32_t seen = 0;
 #pragma unroll
-      for (int kt = 0; kt < 2; ++kt) {
-        f32x4_t s = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int st = 0; st < 4; ++st)
-          s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(kf[kt][st]), as_bf16x8(qb[st]), s, 0, 0, 0);
+      for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const int j = j0 + 16 * kt + 4 * g + r;
           const bool vis = j < L || (TREE && j < end && ((anc >> (j - L)) & 1));
           seen |= (vis ? 1u : 0u) << (4 * kt + r);
-          x[4 * kt + r] = vis ? s[r] * a.scale_log2 : neg_inf();
+          x[4 * kt + r] = vis ? s[kt][nt][r] : neg_inf();
         }
-      }
-      softmax_unit(x, sm[nt], acc[nt], size);
-      const float f = sm[nt].c;
+      softmax_unit(x, sm[nt], acc[nt], a.scale_log2, ls);
       u32x4_t ph, pl;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const float p0 = x[2 * e] * f, p1 = x[2 * e + 1] * f;
+        const float p0 = x[2 * e] * sm[nt].c, p1 = x[2 * e + 1] * sm[nt].c;
         ph[e] = pack_bf16x2(p0, p1);
         pl[e] = pack_bf16x2(p0 - __uint_as_float(ph[e] << 16), p1 - __uint_as_float(ph[e] & 0xffff0000u));
       }
@@ -381,141 +635,208 @@ __global__ __launch_bounds__(kThreads) void q8_attn_kernel(Q8AttnArgs a) {
     }
   }
 
-  // The waves' states join in LDS, a query tile at a time: lane (c, g) holds
-  // row c, dims 32 g + 8 r + t.  Each wave's output enters divided by its own
-  // sum, with the weight 2^(m - M) l.
-  __shared__ float lds_m[kWaves][16], lds_l[kWaves][16];
-  constexpr int kPitch = kD + 4;
-  __shared__ __attribute__((aligned(16))) float lds_o[kWaves][16][kPitch];
+  // From here on q is fp16: of q * 2^(14 - e), e the exponent of the row's largest.
+  float qscale[NT];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int st = 0; st < 4; ++st)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) top = max_size(top, qf[nt][st][e]);
+    const float col = max_across_groups(__uint_as_float(min(larger_half(top), 0x7f7fu) << 16));
+    const int ex = max((int)(__float_as_uint(col) >> 23), 15);  // biased exponent; q * 2^(141 - ex) is below 2^15
+    const float up = __uint_as_float((uint32_t)(268 - ex) << 23);
+    qscale[nt] = a.scale_log2 * __uint_as_float((uint32_t)(ex - 14) << 23);
+#pragma unroll
+    for (int st = 0; st < 4; ++st)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        qf[nt][st][e] = pack_f16x2(__uint_as_float(qf[nt][st][e] << 16) * up, __uint_as_float(qf[nt][st][e] & 0xffff0000u) * up);
+  }
+
+  // Blocks: a stage is loaded again as soon as its codes have been converted.
+  while (u < ue) {
+#pragma unroll
+    for (int stage = 0; stage < kStages; ++stage) {
+      if (u < ue) {
+        const float ks = unit_scale[stage].x, vs = unit_scale[stage].y;
+        const int further = kStages == 1 ? next(u) : next(next(u));
+        unit_scale[stage] = load_scale(further);
+        const __amdgpu_buffer_rsrc_t ahead = unit_rsrc(blocks, further, ue);
+        RawUnit& f = raw[stage];
+        f32x4_t s[2][NT];
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt) {
+          u32x4_t kf[4];
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            kf[2 * h] = decode8<INT8>(f.k[2 * kt + h][0], f.k[2 * kt + h][1]);
+            kf[2 * h + 1] = decode8<INT8>(f.k[2 * kt + h][2], f.k[2 * kt + h][3]);
+          }
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) {
+            f32x4_t x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int st = 0; st < 4; ++st)
+              x = __builtin_amdgcn_mfma_f32_16x16x32_f16(as_f16x8(kf[st]), as_f16x8(qf[nt][st]), x, 0, 0, 0);
+            s[kt][nt] = x;
+          }
+        }
+        load_k<kPolicy>(f, ahead, lane);
+        u32x4_t vf[8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          vf[2 * i] = decode8<INT8>(f.v[i][0], f.v[i][1]);
+          vf[2 * i + 1] = decode8<INT8>(f.v[i][2], f.v[i][3]);
+        }
+        load_v<kPolicy>(f, ahead, lane);
+        const float ls = __builtin_amdgcn_logf(vs);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          float x[8];
+#pragma unroll
+          for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) x[4 * kt + r] = s[kt][nt][r];
+          softmax_unit(x, sm[nt], acc[nt], qscale[nt] * ks, ls);
+          const float w = vs * sm[nt].c;
+          u32x4_t pf;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) pf[e] = pack_f16x2(x[2 * e] * w, x[2 * e + 1] * w);
+#pragma unroll
+          for (int t = 0; t < 8; ++t)
+            acc[nt][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(as_f16x8(vf[t]), as_f16x8(pf), acc[nt][t], 0, 0, 0);
+        }
+        u = next(u);
+      }
+    }
+  }
+
+  // The waves' states join in LDS: first maxima and sums, then every wave's output
+  // times 2^(m - M) / (c L), to be added up.  Lane (c, g) holds row c of each
+  // tile, dims 32 g + 8 r + t.
+  const bool finished = rn.n == 1;
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
     const float l = sum_across_groups(sm[nt].l);
-    if (g == 0) lds_m[wave][c] = sm[nt].m, lds_l[wave][c] = l;
-    const float inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);  // NaN stays
-    const float unit = sm[nt].c > 0.f ? 1.f / sm[nt].c : 0.f;
+    if (g == 0) lds.m[wave][16 * nt + c] = sm[nt].m, lds.l[wave][16 * nt + c] = l;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    float M, Lsum;
+    join_sums<kKeyWaves>(lds, rg * kKeyWaves, 16 * nt + c, M, Lsum);
+    const float part = (sm[nt].m == neg_inf() ? 0.f : fast_exp2(sm[nt].m - M)) * reciprocal(Lsum);
+    const float unit = sm[nt].lc == kNoFactor ? 0.f : fast_exp2(-sm[nt].lc);
 #pragma unroll
     for (int r = 0; r < 4; ++r)
 #pragma unroll
       for (int t = 0; t < 8; t += 4) {
         f32x4_t o;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) o[e] = acc[nt][t + e][r] * inv * unit;
-        *(f32x4_t*)&lds_o[wave][c][32 * g + 8 * r + t] = o;
+        for (int e = 0; e < 4; ++e) o[e] = acc[nt][t + e][r] * part * unit;
+        *(f32x4_t*)&lds.o[wave][16 * nt + c][32 * g + 8 * r + t] = o;
       }
-    __syncthreads();
-    const int row = tid / 16, d = tid % 16 * 8, r = row0 + 16 * nt + row;
-    if (r < R) {
-      float M = neg_inf(), Lsum = 0.f, o[8];
+  }
+  __syncthreads();
+  {
+    constexpr int kTPR = kThreads / kRows, kDims = kD / kTPR;  // threads a row, dims a thread
+    const int in = tid / kTPR, d = tid % kTPR * kDims, r = grp * kRows + in;
+    const int first = in / (16 * NT) * kKeyWaves, row = in % (16 * NT);
+    f32x4_t o[kDims / 4];
 #pragma unroll
-      for (int w = 0; w < kWaves; ++w) M = fmaxf(M, lds_m[w][row]);
+    for (int i = 0; i < kDims / 4; ++i) o[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int e = 0; e < 8; ++e) o[e] = 0.f;
+    for (int w = 0; w < kKeyWaves; ++w)
 #pragma unroll
-      for (int w = 0; w < kWaves; ++w) {
-        const float lw = lds_l[w][row];
-        const float wt = lw == 0.f ? 0.f : fast_exp2(lds_m[w][row] - (M == neg_inf() ? 0.f : M)) * lw;
-        Lsum += wt;
-        if (lw != 0.f)
+      for (int i = 0; i < kDims / 4; ++i) o[i] += *(const f32x4_t*)&lds.o[first + w][row][d + 4 * i];
+    if (r < R && finished) {
+      const int n = r / G;
+      uint16_t* dst = a.out + (((size_t)b * a.N + n) * a.H + hk * G + (r - n * G)) * kD + d;
 #pragma unroll
-          for (int e = 0; e < 8; ++e) o[e] += wt * lds_o[w][row][d + e];
+      for (int i = 0; i < kDims / 4; ++i)
+        *(u32x2_t*)(dst + 4 * i) = u32x2_t{pack_bf16x2(o[i][0], o[i][1]), pack_bf16x2(o[i][2], o[i][3])};
+    } else if (r < R) {
+      const size_t at = ((size_t)run * a.groups + grp) * kRows;
+      if (d == 0) {
+        float M, Lsum;
+        join_sums<kKeyWaves>(lds, first, row, M, Lsum);
+        __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2_t, f32x2_t{M, Lsum}),
+                                              state_rsrc(a.part_ml + at, kRows * 8), in * 8, 0, kDeviceScope);
       }
-      const float inv_l = Lsum > 0.f ? 1.f / Lsum : (Lsum == 0.f ? 0.f : Lsum);
+      const __amdgpu_buffer_rsrc_t ro = state_rsrc(a.part_o + at * kD, kRows * kD * 4);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) o[e] *= inv_l;
-      if (a.splits == 1) {
-        u32x4_t w;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) w[e] = pack_bf16x2(o[2 * e], o[2 * e + 1]);
-        *(u32x4_t*)(a.out + (((size_t)b * a.N + r / G) * a.H + hk * G + r % G) * kD + d) = w;
-      } else {
-        const size_t at = ((head * a.groups + grp) * a.splits + split) * (16 * NT) + 16 * nt + row;
-        if (d == 0) a.part_ml[at] = make_float2(M, Lsum);
-        *(f32x4_t*)(a.part_o + at * kD + d) = f32x4_t{o[0], o[1], o[2], o[3]};
-        *(f32x4_t*)(a.part_o + at * kD + d + 4) = f32x4_t{o[4], o[5], o[6], o[7]};
-      }
+      for (int i = 0; i < kDims / 4; ++i)
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, o[i]), ro, (in * kD + d + 4 * i) * 4, 0,
+                                               kDeviceScope);
     }
-    __syncthreads();
   }
+  if (finished) return;
+  unsigned* counter = a.counters + (head * a.groups + grp) * kCounterStride;
+  if (last_to_arrive(counter, rn.n, &lds.flag))
+    join_states<kRows>(a, rn.first, rn.n, grp, min(kRows, R - grp * kRows),
+                       a.out + ((size_t)b * a.N * a.H + hk * G) * kD, grp * kRows, G, lds);
 }
 
-// Joins the splits' outputs in split order: 16 threads a row.
-template <int NT>
-__global__ __launch_bounds__(kThreads) void q8_attn_combine(Q8AttnArgs a) {
-  const int G = a.H / a.H_kv, R = a.N * G;
-  const size_t id = (size_t)blockIdx.x * 16 + threadIdx.x / 16;
-  const size_t head = id / R;
-  const int r = id % R, d = threadIdx.x % 16 * 8;
-  if (head >= (size_t)a.B * a.H_kv) return;
-  const int grp = r / (16 * NT), in = r % (16 * NT);
-  const size_t first = (head * a.groups + grp) * a.splits * (16 * NT) + in;
-  float M = neg_inf(), L = 0.f, o[8];
-#pragma unroll
-  for (int e = 0; e < 8; ++e) o[e] = 0.f;
-  for (int s = 0; s < a.splits; ++s) M = fmaxf(M, a.part_ml[first + (size_t)s * 16 * NT].x);
-  for (int s = 0; s < a.splits; ++s) {
-    const size_t at = first + (size_t)s * 16 * NT;
-    const float2 ml = a.part_ml[at];
-    if (ml.y == 0.f) continue;
-    const float w = fast_exp2(ml.x - (M == neg_inf() ? 0.f : M)) * ml.y;
-    L += w;
-    const f32x4_t x = *(const f32x4_t*)(a.part_o + at * kD + d), y = *(const f32x4_t*)(a.part_o + at * kD + d + 4);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) o[e] += w * x[e], o[4 + e] += w * y[e];
-  }
-  const float inv = L > 0.f ? 1.f / L : (L == 0.f ? 0.f : L);
-  u32x4_t w;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) w[e] = pack_bf16x2(o[2 * e] * inv, o[2 * e + 1] * inv);
-  const int b = head / a.H_kv, hk = head % a.H_kv;
-  *(u32x4_t*)(a.out + (((size_t)b * a.N + r / G) * a.H + hk * G + r % G) * kD + d) = w;
-}
-
-template <int NT, bool INT8>
-void launch_nt(const Q8AttnArgs& a, hipStream_t stream) {
-  const dim3 grid(a.H_kv * a.groups, a.B, a.splits), block(kThreads);
+template <int NT, int RG, bool INT8>
+void launch_type(const Q8AttnArgs& a, hipStream_t stream) {
+  const long runs = a.groups == 1 ? a.runs : (a.runs + 7) / 8 * 8;
+  const dim3 grid((unsigned)runs * a.groups), block(kThreads);
   if (a.parents)
-    hipLaunchKernelGGL((q8_attn_kernel<NT, INT8, true>), grid, block, 0, stream, a);
+    hipLaunchKernelGGL((q8_attn_kernel<NT, RG, INT8, true>), grid, block, 0, stream, a);
   else
-    hipLaunchKernelGGL((q8_attn_kernel<NT, INT8, false>), grid, block, 0, stream, a);
+    hipLaunchKernelGGL((q8_attn_kernel<NT, RG, INT8, false>), grid, block, 0, stream, a);
 }
 
-template <int NT>
-hipError_t launch_tiles(const Q8AttnArgs& a, bool int8, hipStream_t stream) {
+template <int NT, int RG>
+hipError_t launch_rows(const Q8AttnArgs& a, bool int8, hipStream_t stream) {
   if (int8)
-    launch_nt<NT, true>(a, stream);
+    launch_type<NT, RG, true>(a, stream);
   else
-    launch_nt<NT, false>(a, stream);
-  const hipError_t e = hipGetLastError();
-  if (e != hipSuccess || a.splits == 1) return e;
-  const size_t rows = (size_t)a.B * a.N * a.H;
-  hipLaunchKernelGGL((q8_attn_combine<NT>), dim3((rows + 15) / 16), dim3(kThreads), 0, stream, a);
+    launch_type<NT, RG, false>(a, stream);
   return hipGetLastError();
 }
 
 }  // namespace
 
+constexpr int kMinUnits = 4 * kWaves;  // units of a run at least
+// Pairs from which on no pair is split: the waves of half of the CUs draw the
+// whole memory bandwidth, and a split's states cost some microseconds.
+constexpr int kUnsplit = kNumCU / 2;
+
 Q8AttnPlan plan_q8_attn(int B, int N, int H, int H_kv, int n_blocks, int max_splits) {
   Q8AttnPlan p{};
   const int R = N * (H / H_kv);
-  p.tiles = R <= 16 ? 1 : (R <= 32 ? 2 : 4);
-  p.groups = (R + 16 * p.tiles - 1) / (16 * p.tiles);
-  const long wgs = (long)B * H_kv * p.groups;
-  const int most = max(1, min(kMaxSplits, n_blocks / 4));
-  const int want = max_splits > 0 ? max_splits : (int)min((2L * kNumCU + wgs - 1) / wgs, (long)kMaxSplits);
-  p.splits = max(1, min(want, most));
-  if (p.splits > 1) {
-    const size_t rows = (size_t)wgs * p.splits * 16 * p.tiles;
-    p.part_ml_off = kCounterBytes;  // the counters of a shared workspace stay as they are
-    p.part_o_off = (p.part_ml_off + rows * sizeof(float2) + 255) & ~(size_t)255;
-    p.ws_bytes = p.part_o_off + rows * kD * sizeof(float);
+  p.rows = R <= 16 ? 16 : (R <= 32 ? 32 : 64);
+  p.groups = (R + p.rows - 1) / p.rows;
+  const long pairs = (long)B * H_kv, most = n_blocks + (kQ8Block - 1 + N + kQ8Block - 1) / kQ8Block;
+  // more pairs than counters are not split: they fill the GPU by themselves
+  if (pairs * p.groups > kCounterSlots || max_splits == 1 ||
+      (max_splits == 0 && (most <= kMinUnits || pairs * p.groups >= kUnsplit))) {
+    p.splits = 1;
+    p.runs = pairs;
+    return p;
   }
+  if (max_splits > 0) {
+    p.splits = (int)min((long)max_splits, most);
+    p.runs = pairs * p.splits;
+  } else {
+    p.min_units = kMinUnits;
+    p.target = max(1, kNumCU / p.groups);
+    p.runs = pairs + min((long)p.target, pairs * most / kMinUnits);
+  }
+  const size_t states = (size_t)p.runs * p.groups * p.rows;
+  p.part_ml_off = kCounterBytes;
+  p.part_o_off = (p.part_ml_off + states * sizeof(float2) + 255) & ~(size_t)255;
+  p.ws_bytes = p.part_o_off + states * kD * sizeof(float);
   return p;
 }
 
-hipError_t launch_q8_attn(const Q8AttnArgs& a, bool int8, int tiles, hipStream_t stream) {
-  if (tiles == 1) return launch_tiles<1>(a, int8, stream);
-  if (tiles == 2) return launch_tiles<2>(a, int8, stream);
-  return launch_tiles<4>(a, int8, stream);
+hipError_t launch_q8_attn(const Q8AttnArgs& a, bool int8, int rows, hipStream_t stream) {
+  if (rows == 16) return launch_rows<1, 1>(a, int8, stream);
+  if (rows == 32) return launch_rows<2, 1>(a, int8, stream);
+  return launch_rows<2, 2>(a, int8, stream);
 }
 
 }  // namespace glide
