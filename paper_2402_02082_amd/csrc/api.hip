@@ -657,7 +657,7 @@ int glide_q8_tree_attn(const void* q, const glide_q8_cache* cache, const int32_t
   a.runs = (int)p.runs;
   const double sc = scale > 0.f ? (double)scale : 1.0 / sqrt((double)D);
   a.scale_log2 = (float)(sc * 1.4426950408889634);  // log2(e)
-  return hip_status(glide::launch_q8_attn(a, kind == GLIDE_INT8, p.rows, stream));
+  return hip_status(glide::launch_q8_attn(a, kind == GLIDE_INT8, p.rows, p.waves, stream));
 }
 
 int glide_q8_commit(const glide_q8_cache* caches, int layers, const int32_t* seq_lens,

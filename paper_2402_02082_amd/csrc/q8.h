@@ -76,13 +76,13 @@ struct Q8CommitArgs {
 };
 hipError_t launch_q8_commit(const Q8CommitArgs& a, bool int8, hipStream_t stream);
 
-// How the attention over an 8-bit cache is divided: workgroups of `rows` query
-// rows, `groups` of them over the rows of a cached head, and its keys in runs of
-// units -- `splits` of every pair (sequence, cached head), or with splits == 0
-// about `target` of equal size in all, of at least min_units units each.  runs:
-// at most so many.
+// How the attention over an 8-bit cache is divided: workgroups of `waves` waves
+// for `rows` query rows, `groups` of them over the rows of a cached head, and its
+// keys in runs of units -- `splits` of every pair (sequence, cached head), or
+// with splits == 0 up to `target` of equal size in all, of at least min_units
+// units each.  runs: at most so many.
 struct Q8AttnPlan {
-  int rows, groups, splits, target, min_units;
+  int rows, groups, waves, splits, target, min_units;
   long runs;
   size_t ws_bytes, part_ml_off, part_o_off;
 };
@@ -100,7 +100,7 @@ struct Q8AttnArgs {
   int B, N, H, H_kv, n_blocks, groups, splits, target, min_units, runs;
   float scale_log2;
 };
-hipError_t launch_q8_attn(const Q8AttnArgs& a, bool int8, int rows, hipStream_t stream);
+hipError_t launch_q8_attn(const Q8AttnArgs& a, bool int8, int rows, int waves, hipStream_t stream);
 
 // Rotary positions of queries and keys.
 struct RopeRows {

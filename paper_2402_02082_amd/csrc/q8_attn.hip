@@ -14,9 +14,10 @@
 // there; of the others each run leaves a state, counts itself in, and the one
 // that completes the pair joins the states in order, whichever that is: one
 // launch.
-// A workgroup's eight waves take units in turn, each for all of the group's rows
-// (up to 32 rows; 64 rows: four waves for each half, the second read of a unit
-// then comes from L2), so each code is converted by one or two waves.
+// A workgroup's waves (eight, or four where pairs are split) take units in turn,
+// each for all of the group's rows (up to 32 rows; 64 rows: four waves for each
+// half, the second read of a unit then comes from L2), so each code is converted
+// by one or two waves.
 //
 // Per unit and wave, on v_mfma_f32_16x16x32:
 //   S^T[key, query] = K Q^T, softmax on S^T with one query per lane column,
@@ -50,8 +51,6 @@ typedef __attribute__((ext_vector_type(4))) float f32x4_t;
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4_t;
 
 constexpr int kD = kHeadDim;
-constexpr int kWaves = 8;
-constexpr int kThreads = 64 * kWaves;
 
 __device__ __forceinline__ float neg_inf() { return -__builtin_huge_valf(); }
 __device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -140,6 +139,11 @@ __device__ __forceinline__ uint64_t ancestor_mask(int p, int lane) {
   return ((uint64_t)hi << 32) | lo;
 }
 
+constexpr int kWholeUnits = 24;  // a pair of so few units is not split: joining would cost more than it saves
+// Up to one run a CU, but two from so many units a run on (7B layer of 2048
+// tokens: 8 runs a pair 10.4 us, 9 14.4; one head group of 60000 tokens, 32 runs a
+// pair 25.7, 63 28.2; 128 pairs of 160 units 36.8 with one, 35.0 with two).
+constexpr int kLongRun = 32;
 constexpr int kRingCost = 4;  // blocks that take a wave about as long as a unit of ring rows
 
 constexpr float kRescaleSlack = 8.f;  // how far a score may pass the reference maximum (log2)
@@ -284,13 +288,28 @@ struct Run {
   int b, hk, u0, u1, n, first;
 };
 
-// Runs of a sequence of so many units.
+// Runs of a pair of so many units, of up to `per` units each.
 __device__ __forceinline__ int runs_of(const Q8AttnArgs& a, int units, int per) {
-  return a.splits ? a.splits : (units + per - 1) / per;
+  return a.splits ? a.splits : (units <= kWholeUnits ? 1 : (units + per - 1) / per);
 }
 
-// Run number `run`; false past the last.  Called by whole waves; sequences are
-// looked through 64 at a time, one a lane.
+// Units of sequence b, 0 past the last; `mine`: of the lane's among the first 64.
+__device__ __forceinline__ int units_at(const Q8AttnArgs& a, bool tree, int b, int lane, int mine) {
+  return b == lane ? mine : (b < a.B ? sequence(a, tree, b).units : 0);
+}
+
+// Sum over all sequences of their units (per == 0) or runs.  Called by whole
+// waves; sequences are looked through 64 at a time, one a lane.
+__device__ __forceinline__ int sum_of(const Q8AttnArgs& a, bool tree, int per, int lane, int mine) {
+  int sum = 0;
+  for (int b0 = 0; b0 < a.B; b0 += 64) {
+    const int units = units_at(a, tree, b0 + lane, lane, mine);
+    sum += per == 0 || units == 0 ? units : runs_of(a, units, per);
+  }
+  return __builtin_amdgcn_readlane(scan64(sum), 63);
+}
+
+// Run number `run`; false past the last.  Called by whole waves.
 __device__ __forceinline__ bool find_run(const Q8AttnArgs& a, bool tree, int run, int lane, Run* r) {
   int b = 0, before = 0, per = 1;
   if (a.splits) {
@@ -310,16 +329,22 @@ __device__ __forceinline__ bool find_run(const Q8AttnArgs& a, bool tree, int run
     }
   } else if (a.B == 1) {
     const int units = sequence(a, tree, 0).units;
-    per = max((units * a.H_kv + a.target - 1) / a.target, a.min_units);
+    const int most = units * a.H_kv >= a.target * kLongRun ? a.target : (a.target + 1) / 2, n = max(1, most / a.H_kv);
+    per = max((units + n - 1) / n, a.min_units);
   } else {
-    int total = 0;
-    for (int b0 = 0; b0 < a.B; b0 += 64) total += b0 + lane < a.B ? sequence(a, tree, b0 + lane).units : 0;
-    total = __builtin_amdgcn_readlane(scan64(total), 63);
-    per = max((total * a.H_kv + a.target - 1) / a.target, a.min_units);
+    // about the fewest units a run with which no more than `most` runs come out:
+    // n pairs of any lengths have about n / 2 runs more than whole ones would be
+    const int mine = lane < a.B ? sequence(a, tree, lane).units : 0;
+    const int total = sum_of(a, tree, 0, lane, mine) * a.H_kv;
+    const int most = total >= a.target * kLongRun ? a.target : (a.target + 1) / 2;
+    const int whole = max(1, most - a.B * a.H_kv / 2);
+    per = max((total + whole - 1) / whole, a.min_units);
+    for (int i = 0; i < 16 && sum_of(a, tree, per, lane, mine) * a.H_kv > most; ++i) per += (per + 7) / 8;
     int sum = 0;
     bool found = false;
     for (int b0 = 0; b0 < a.B && !found; b0 += 64) {
-      const int n = b0 + lane < a.B ? runs_of(a, sequence(a, tree, b0 + lane).units, per) * a.H_kv : 0;
+      const int units = units_at(a, tree, b0 + lane, lane, mine);
+      const int n = units ? runs_of(a, units, per) * a.H_kv : 0;
       const int incl = sum + scan64(n);
       const uint64_t hit = __ballot(run < incl);
       found = hit != 0;
@@ -364,10 +389,10 @@ __device__ __forceinline__ bool last_to_arrive(unsigned* counter, int n, int* fl
 }
 
 constexpr int kPitch = kD + 4;  // floats between LDS rows, so that rows start in other banks
-template <int ROWS>  // query rows of a wave
+template <int WAVES, int ROWS>  // query rows of a wave
 struct JoinLds {
-  float m[kWaves][ROWS], l[kWaves][ROWS];
-  __attribute__((aligned(16))) float o[kWaves][ROWS][kPitch];
+  float m[WAVES][ROWS], l[WAVES][ROWS];
+  __attribute__((aligned(16))) float o[WAVES][ROWS][kPitch];
   int flag;
 };
 
@@ -392,16 +417,16 @@ __device__ __forceinline__ void join_sums(const Lds& lds, int first, int row, fl
 // The states of a pair joined in run order into output rows.  State i of n is in
 // the slot of its run, first + i * H_kv; `rows` of the group's kRows are in use.  16 lanes take a row, so a wave takes four at a time; where
 // the rows do not fill the waves, several waves share a row's states.
-template <int kRows, class Lds>
+template <int WAVES, int kRows, class Lds>
 __device__ __forceinline__ void join_states(const Q8AttnArgs& a, int first, int n, int grp, int rows, uint16_t* out,
                                             int row_first, int G, Lds& lds) {
   constexpr int kBatch = 8;  // states requested at once
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int quads = (rows + 3) / 4;
-  const int parts = quads == 1 ? 8 : (quads == 2 ? 4 : (quads <= 4 ? 2 : 1));  // waves that share a row
+  const int parts = quads == 1 ? WAVES : (quads == 2 ? WAVES / 2 : (quads <= 4 ? WAVES / 4 : 1));  // waves that share a row
   const int part = wave % parts, d = lane % 16 * 8;
-  for (int quad = wave / parts; quad < quads; quad += kWaves / parts) {
+  for (int quad = wave / parts; quad < quads; quad += WAVES / parts) {
     const int row = 4 * quad + lane / 16;
     const bool live = row < rows;
     float M = neg_inf(), L = 0.f, o[8];
@@ -464,9 +489,11 @@ __device__ __forceinline__ void join_states(const Q8AttnArgs& a, int first, int 
   }
 }
 
-template <int NT, int RG, bool INT8, bool TREE>
-__global__ __launch_bounds__(kThreads) void q8_attn_kernel(Q8AttnArgs a) {
-  constexpr int kKeyWaves = kWaves / RG;
+template <int WAVES, int NT, int RG, bool INT8, bool TREE>
+__global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2)))
+void q8_attn_kernel(Q8AttnArgs a) {
+  constexpr int kThreads = 64 * WAVES;
+  constexpr int kKeyWaves = WAVES / RG;
   constexpr int kStages = NT == 1 ? 2 : 1;
   constexpr int kPolicy = RG == 1 ? kStream : kKeep;
   constexpr int kRows = 16 * NT * RG;  // query rows of a workgroup
@@ -478,7 +505,7 @@ __global__ __launch_bounds__(kThreads) void q8_attn_kernel(Q8AttnArgs a) {
   const int grp = a.groups == 1 ? 0 : blockIdx.x / 8 % a.groups;
   const int run = a.groups == 1 ? blockIdx.x : blockIdx.x / (8 * a.groups) * 8 + blockIdx.x % 8;
   const int G = a.H / a.H_kv, R = a.N * G, row0 = grp * kRows + rg * 16 * NT;
-  __shared__ JoinLds<16 * NT> lds;
+  __shared__ JoinLds<WAVES, 16 * NT> lds;
 
   Run rn;
   if (!find_run(a, TREE, run, lane, &rn)) return;
@@ -775,56 +802,57 @@ __global__ __launch_bounds__(kThreads) void q8_attn_kernel(Q8AttnArgs a) {
   if (finished) return;
   unsigned* counter = a.counters + (head * a.groups + grp) * kCounterStride;
   if (last_to_arrive(counter, rn.n, &lds.flag))
-    join_states<kRows>(a, rn.first, rn.n, grp, min(kRows, R - grp * kRows),
+    join_states<WAVES, kRows>(a, rn.first, rn.n, grp, min(kRows, R - grp * kRows),
                        a.out + ((size_t)b * a.N * a.H + hk * G) * kD, grp * kRows, G, lds);
 }
 
-template <int NT, int RG, bool INT8>
-void launch_type(const Q8AttnArgs& a, hipStream_t stream) {
-  const long runs = a.groups == 1 ? a.runs : (a.runs + 7) / 8 * 8;
-  const dim3 grid((unsigned)runs * a.groups), block(kThreads);
-  if (a.parents)
-    hipLaunchKernelGGL((q8_attn_kernel<NT, RG, INT8, true>), grid, block, 0, stream, a);
-  else
-    hipLaunchKernelGGL((q8_attn_kernel<NT, RG, INT8, false>), grid, block, 0, stream, a);
-}
-
-template <int NT, int RG>
+template <int WAVES, int NT, int RG>
 hipError_t launch_rows(const Q8AttnArgs& a, bool int8, hipStream_t stream) {
-  if (int8)
-    launch_type<NT, RG, true>(a, stream);
+  const long runs = a.groups == 1 ? a.runs : (a.runs + 7) / 8 * 8;
+  const dim3 grid((unsigned)(runs * a.groups)), block(64 * WAVES);
+  if (a.parents && int8)
+    hipLaunchKernelGGL((q8_attn_kernel<WAVES, NT, RG, true, true>), grid, block, 0, stream, a);
+  else if (a.parents)
+    hipLaunchKernelGGL((q8_attn_kernel<WAVES, NT, RG, false, true>), grid, block, 0, stream, a);
+  else if (int8)
+    hipLaunchKernelGGL((q8_attn_kernel<WAVES, NT, RG, true, false>), grid, block, 0, stream, a);
   else
-    launch_type<NT, RG, false>(a, stream);
+    hipLaunchKernelGGL((q8_attn_kernel<WAVES, NT, RG, false, false>), grid, block, 0, stream, a);
   return hipGetLastError();
 }
 
 }  // namespace
 
-constexpr int kMinUnits = 4 * kWaves;  // units of a run at least
-// Pairs from which on no pair is split: the waves of half of the CUs draw the
-// whole memory bandwidth, and a split's states cost some microseconds.
-constexpr int kUnsplit = kNumCU / 2;
+// Pairs up to which pairs are split.  The eight waves of a pair on half of the
+// CUs draw the whole memory bandwidth, and joining splits takes 3 us (13B layer,
+// 160 pairs: one run a pair 28 us, two 35 us); 128 pairs of unequal length are
+// faster in up to 512 runs of four waves (46 against 37 us).
+constexpr int kMostSplit = kNumCU / 2;
+constexpr int kMinUnits = 8;  // units of a run at least, of pairs that are split
 
 Q8AttnPlan plan_q8_attn(int B, int N, int H, int H_kv, int n_blocks, int max_splits) {
   Q8AttnPlan p{};
   const int R = N * (H / H_kv);
   p.rows = R <= 16 ? 16 : (R <= 32 ? 32 : 64);
   p.groups = (R + p.rows - 1) / p.rows;
+  p.waves = 8;
   const long pairs = (long)B * H_kv, most = n_blocks + (kQ8Block - 1 + N + kQ8Block - 1) / kQ8Block;
-  // more pairs than counters are not split: they fill the GPU by themselves
-  if (pairs * p.groups > kCounterSlots || max_splits == 1 ||
-      (max_splits == 0 && (most <= kMinUnits || pairs * p.groups >= kUnsplit))) {
+  // (pairs past the counters are not split either way)
+  if (max_splits == 1 || most == 1 || pairs * p.groups > (max_splits ? kCounterSlots : kMostSplit)) {
     p.splits = 1;
     p.runs = pairs;
     return p;
   }
+  // 64 rows take eight waves, one workgroup a CU; fewer rows four waves, two
+  if (p.rows < 64) p.waves = 4;
   if (max_splits > 0) {
     p.splits = (int)min((long)max_splits, most);
     p.runs = pairs * p.splits;
   } else {
     p.min_units = kMinUnits;
-    p.target = max(1, kNumCU / p.groups);
-    p.runs = pairs + min((long)p.target, pairs * most / kMinUnits);
+    p.target = max(1, 2 * kNumCU / p.groups);
+    p.runs = max(pairs, min(pairs + p.target, pairs * ((most + kMinUnits - 1) / kMinUnits)));
+    if (most <= kWholeUnits) return p;  // no pair will be split: no states
   }
   const size_t states = (size_t)p.runs * p.groups * p.rows;
   p.part_ml_off = kCounterBytes;
@@ -833,10 +861,10 @@ Q8AttnPlan plan_q8_attn(int B, int N, int H, int H_kv, int n_blocks, int max_spl
   return p;
 }
 
-hipError_t launch_q8_attn(const Q8AttnArgs& a, bool int8, int rows, hipStream_t stream) {
-  if (rows == 16) return launch_rows<1, 1>(a, int8, stream);
-  if (rows == 32) return launch_rows<2, 1>(a, int8, stream);
-  return launch_rows<2, 2>(a, int8, stream);
+hipError_t launch_q8_attn(const Q8AttnArgs& a, bool int8, int rows, int waves, hipStream_t stream) {
+  if (rows == 16) return waves == 4 ? launch_rows<4, 1, 1>(a, int8, stream) : launch_rows<8, 1, 1>(a, int8, stream);
+  if (rows == 32) return waves == 4 ? launch_rows<4, 2, 1>(a, int8, stream) : launch_rows<8, 2, 1>(a, int8, stream);
+  return launch_rows<8, 2, 2>(a, int8, stream);
 }
 
 }  // namespace glide
