@@ -9,6 +9,11 @@
 // of a verification step, and fewer than 32 accepted rows behind the last
 // whole block -- stay bfloat16 in the ring, so a rejected token never touches
 // a scale and nothing is quantised twice.
+//
+// One wave takes one block of one head, without barriers: its lanes load the values that their units of the block hold (K: 16 dims of a
+// token; V: eight dims of eight tokens), so that the transposed V is a matter of
+// byte order in registers, and every store is 1 KB in a row.  Four waves of a
+// workgroup take neighbouring heads, whose rows of a token lie together.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -20,99 +25,133 @@ namespace {
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2_t;
 typedef __attribute__((ext_vector_type(2))) float f32x2_t;
 typedef __attribute__((ext_vector_type(4))) float f32x4_t;
-typedef __attribute__((ext_vector_type(2))) uint32_t u32x2_t;
+typedef __attribute__((ext_vector_type(2))) uint16_t u16x2_t;
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4_t;
 
-constexpr int kThreads = 256;
+constexpr int kWaves = 4;
+constexpr int kThreads = 64 * kWaves;
 constexpr int kChunks = kHeadDim / 8;  // 16-byte pieces of a bf16 row
 
 __device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
   f32x2_t f = {lo, hi};
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(f, bf16x2_t));
 }
+__device__ __forceinline__ float low_half(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float high_half(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
 
-// Scales below the smallest normal number count as 0: their block is zeros.
-constexpr float kTinyScale = 1.17549435e-38f;
-
-template <bool INT8>
-__device__ __forceinline__ float scale_of(uint32_t amax_bits) {
-  const float s = __uint_as_float(amax_bits << 16) / (INT8 ? 127.f : 448.f);
-  return s < kTinyScale ? 0.f : s;
+// The larger magnitude of each half, as bits (their order is that of the sizes,
+// with NaN above all), and the maximum over a wave.
+__device__ __forceinline__ uint32_t max_size(uint32_t top, uint32_t bf16s) {
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2_t, top),
+                                                                __builtin_bit_cast(u16x2_t, bf16s & 0x7fff7fffu)));
+}
+template <int CTRL>
+__device__ __forceinline__ uint32_t max_moved(uint32_t v) {
+  return max(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, CTRL, 0xF, 0xF, true));
+}
+__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
+  v = max_moved<0x140>(max_moved<0x141>(max_moved<0x4E>(max_moved<0xB1>(v))));
+  return max(max(__builtin_amdgcn_readlane(v, 0), __builtin_amdgcn_readlane(v, 16)),
+             max(__builtin_amdgcn_readlane(v, 32), __builtin_amdgcn_readlane(v, 48)));
 }
 
-// Codes of four values (already divided), one byte each.
+// x / scale, rounded like the division itself, for a whole block's x.  With the
+// scale's rounded reciprocal, a first correction by the remainder brings the
+// quotient within one unit of the last place, and a second one, whose remainder
+// is exact then, gives the rounded quotient (Markstein, 1990; five operations a
+// value where a division takes about ten).  A scale below the smallest normal
+// number counts as 0.
+struct Divider {
+  float s, inv;
+  __device__ __forceinline__ float operator()(float x) const {
+    float q = x * inv;
+    q = fmaf(fmaf(-q, s, x), inv, q);
+    return fmaf(fmaf(-q, s, x), inv, q);
+  }
+};
+
+// Codes of four values (already divided), one byte each.  A quotient passes the
+// largest code by a few units of the last place at most, and rounds to it.
+// int8: added to 1.5 * 2^23 + 128 a value is rounded to an integer, ties to even,
+// which the sum's low byte holds.
 template <bool INT8>
 __device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d) {
-  constexpr float kMost = INT8 ? 127.f : 448.f;
-  a = fminf(fmaxf(a, -kMost), kMost), b = fminf(fmaxf(b, -kMost), kMost);
-  c = fminf(fmaxf(c, -kMost), kMost), d = fminf(fmaxf(d, -kMost), kMost);
   if (INT8) {
-    const uint32_t w = (uint32_t)((int)rintf(a) + 128) | (uint32_t)((int)rintf(b) + 128) << 8;
-    return w | (uint32_t)((int)rintf(c) + 128) << 16 | (uint32_t)((int)rintf(d) + 128) << 24;
+    constexpr float kShift = 12583040.f;
+    const uint32_t lo = __builtin_amdgcn_perm(__float_as_uint(b + kShift), __float_as_uint(a + kShift), 0x0c0c0400u);
+    const uint32_t hi = __builtin_amdgcn_perm(__float_as_uint(d + kShift), __float_as_uint(c + kShift), 0x04000c0cu);
+    return lo | hi;
   }
   int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
   w = __builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
   return (uint32_t)w;
 }
 
-struct BlockLds {
-  uint32_t amax[2][kThreads / 64];
-  __attribute__((aligned(16))) uint8_t codes[kQ8BlockBytes];
-};
-
-// Quantises a block and writes it: the thread holds 16-byte chunks tid and
-// tid + 256 (row chunk / 16, dims 8 (chunk % 16) ..) of K (x[0]) and V (x[1]).
-// Called by the whole workgroup; the codes gather in LDS in the block's byte
-// order and leave it 16 bytes a lane.
-template <bool INT8>
-__device__ __forceinline__ void quantise_block(const u32x4_t (&x)[2][2], uint8_t* block, float* scales, BlockLds& lds) {
-  const int tid = threadIdx.x;
+// Quantises and writes K or V of a block, called by a whole wave; row(t) is where
+// token t's values start.  Lane 16 g + c takes of K, for each (kt, h), token
+// 16 kt + c, dims 64 h + 16 g + (0..15): x[4 kt + 2 h + half]; of V the tokens
+// 16 (i / 4) + 4 g + i % 4, dims 8 c + (0..7): x[i].
+template <bool INT8, class Row>
+__device__ __forceinline__ void quantise_part(bool v, int lane, uint8_t* part, float* scale_out, Row row) {
+  const int c = lane & 15, g = lane >> 4;
+  u32x4_t x[8];
+  if (v) {
 #pragma unroll
-  for (int m = 0; m < 2; ++m) {
-    uint32_t top = 0;  // |x| as bits: their order is that of the magnitudes, NaN above all
+    for (int i = 0; i < 8; ++i) x[i] = *(const u32x4_t*)(row(16 * (i >> 2) + 4 * g + (i & 3)) + 8 * c);
+  } else {
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
+    for (int kt = 0; kt < 2; ++kt) {
+      const uint16_t* p = row(16 * kt + c) + 16 * g;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        top = max(top, x[m][j][e] & 0x7fffu);
-        top = max(top, (x[m][j][e] >> 16) & 0x7fffu);
-      }
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, d));
-    if ((tid & 63) == 0) lds.amax[m][tid >> 6] = top;
-  }
-  __syncthreads();
-#pragma unroll
-  for (int m = 0; m < 2; ++m) {
-    uint32_t top = 0;
-#pragma unroll
-    for (int w = 0; w < kThreads / 64; ++w) top = max(top, lds.amax[m][w]);
-    const float s = scale_of<INT8>(top);
-    if (tid == 0) scales[m] = s;
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const int chunk = tid + kThreads * j, row = chunk / kChunks, dim = chunk % kChunks * 8;
-      float y[8];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        y[2 * e] = s == 0.f ? 0.f : __uint_as_float(x[m][j][e] << 16) / s;
-        y[2 * e + 1] = s == 0.f ? 0.f : __uint_as_float(x[m][j][e] & 0xffff0000u) / s;
-      }
-      const u32x2_t w = {codes4<INT8>(y[0], y[1], y[2], y[3]), codes4<INT8>(y[4], y[5], y[6], y[7])};
-      if (m == 0) {
-        *(u32x2_t*)(lds.codes + q8_k_byte(row, dim)) = w;
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          lds.codes[kQ8PartBytes + q8_v_byte(row, dim + e)] = (uint8_t)(w[e >> 2] >> (8 * (e & 3)));
-      }
+      for (int i = 0; i < 4; ++i) x[4 * kt + i] = *(const u32x4_t*)(p + 64 * (i >> 1) + 8 * (i & 1));
     }
   }
-  __syncthreads();
+  uint32_t top = 0;
 #pragma unroll
-  for (int m = 0; m < 2; ++m) {
-    const int at = m * kQ8PartBytes + tid * 16;
-    *(u32x4_t*)(block + at) = *(const u32x4_t*)(lds.codes + at);
+  for (int i = 0; i < 8; ++i)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) top = max_size(top, x[i][e]);
+  top = wave_max(max(top & 0xffffu, top >> 16));
+
+  constexpr float kTiny = 1.17549435e-38f, kSmall = 8.67361738e-19f;  // 2^-126, 2^-60
+  float scale = __uint_as_float(top << 16) / (INT8 ? 127.f : 448.f);
+  if (scale < kTiny) scale = 0.f;
+  if (lane == 0) *scale_out = scale;
+  Divider d{scale, scale == 0.f ? 0.f : 1.f / scale};
+  if (scale < kSmall && scale != 0.f) {
+    // x and scale times 2^64, so that remainders are no denormals (of quotients
+    // large enough for a code that is not 0)
+    constexpr float kUp = 18446744073709551616.f;
+    d = Divider{scale * kUp, 1.f / (scale * kUp)};
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[i][e] = pack_bf16x2(low_half(x[i][e]) * kUp, high_half(x[i][e]) * kUp);
+  }
+
+  if (v) {
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      u32x4_t w;
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const uint32_t t0 = x[4 * j][u], t1 = x[4 * j + 1][u], t2 = x[4 * j + 2][u], t3 = x[4 * j + 3][u];
+        w[j] = codes4<INT8>(d(low_half(t0)), d(low_half(t1)), d(low_half(t2)), d(low_half(t3)));
+        w[2 + j] = codes4<INT8>(d(high_half(t0)), d(high_half(t1)), d(high_half(t2)), d(high_half(t3)));
+      }
+      *(u32x4_t*)(part + 1024 * u + 16 * lane) = w;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      u32x4_t w;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const uint32_t lo = x[2 * i + (q >> 1)][2 * (q & 1)], hi = x[2 * i + (q >> 1)][2 * (q & 1) + 1];
+        w[q] = codes4<INT8>(d(low_half(lo)), d(high_half(lo)), d(low_half(hi)), d(high_half(hi)));
+      }
+      *(u32x4_t*)(part + 1024 * i + 16 * lane) = w;
+    }
   }
 }
 
@@ -120,43 +159,46 @@ __device__ __forceinline__ uint16_t* ring(const Q8Cache& c, size_t head, int m) 
   return c.tail + head * kQ8TailElems + m * (kQ8Tail * kHeadDim);
 }
 
-template <bool INT8, bool HOLD>
+// Final rows: workgroup (block of the call, four heads of K or V, sequence).
+template <bool INT8>
 __global__ __launch_bounds__(kThreads) void q8_append_kernel(Q8AppendArgs a) {
-  const int i = blockIdx.x, h = blockIdx.y, b = blockIdx.z, tid = threadIdx.x;
+  const int i = blockIdx.x, b = blockIdx.z, lane = threadIdx.x & 63, m = blockIdx.y & 1;
+  const int h = kWaves * (blockIdx.y >> 1) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (h >= a.H) return;
   const int cap = a.n_blocks * kQ8Block;
   const int L = min(max(a.seq_lens[b], 0), cap);
-  int n = a.counts ? min(max(a.counts[b], 0), a.T) : a.T;
-  if (!HOLD) n = min(n, cap - L);
-  const int end = L + n;
+  const int n = min(a.counts ? min(max(a.counts[b], 0), a.T) : a.T, cap - L);
+  const int end = L + n, block = L / kQ8Block + i;
   const size_t head = (size_t)b * a.H + h;
-  const int64_t from = b * a.sb + h * a.sh;
-  const int block = L / kQ8Block + i;
-  if (!HOLD && (block + 1) * kQ8Block <= end) {
-    __shared__ BlockLds lds;
-    u32x4_t x[2][2];
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const int chunk = tid + kThreads * j, tok = block * kQ8Block + chunk / kChunks, dim = chunk % kChunks * 8;
-#pragma unroll
-      for (int m = 0; m < 2; ++m) {
-        const uint16_t* src = tok < L ? ring(a.cache, head, m) + (tok & (kQ8Tail - 1)) * kHeadDim
-                                      : (m ? a.v : a.k) + from + (tok - L) * a.st;
-        x[m][j] = *(const u32x4_t*)(src + dim);
-      }
-    }
+  const uint16_t* from = (m ? a.v : a.k) + b * a.sb + h * a.sh;
+  uint16_t* held = ring(a.cache, head, m);
+  if ((block + 1) * kQ8Block <= end) {
     const size_t at = head * a.n_blocks + block;
-    quantise_block<INT8>(x, a.cache.blocks + at * kQ8BlockBytes, a.cache.scales + at * 2, lds);
+    quantise_part<INT8>(m, lane, a.cache.blocks + at * kQ8BlockBytes + m * kQ8PartBytes, a.cache.scales + at * 2 + m,
+                        [&](int t) {
+                          const int tok = block * kQ8Block + t;
+                          return tok < L ? held + (tok & (kQ8Tail - 1)) * kHeadDim : from + (tok - L) * a.st;
+                        });
   }
   if (i > 0) return;
-  // the rows behind the last whole block; the first block's workgroup writes
-  // them, once it has read the ring rows that they may take the place of
-  const int t0 = HOLD ? 0 : max(L, end / kQ8Block * kQ8Block) - L;
-  __syncthreads();
-  for (int u = tid; u < 2 * (n - t0) * kChunks; u += kThreads) {
-    const int m = u & 1, t = t0 + (u >> 1) / kChunks, dim = (u >> 1) % kChunks * 8;
-    const u32x4_t x = *(const u32x4_t*)((m ? a.v : a.k) + from + t * a.st + dim);
-    *(u32x4_t*)(ring(a.cache, head, m) + ((L + t) & (kQ8Tail - 1)) * kHeadDim + dim) = x;
+  // The rows behind the last whole block; the wave of the first block writes
+  // them, behind its own reads of ring rows that they may take the place of.
+  const int t0 = max(L, end / kQ8Block * kQ8Block) - L;
+  for (int u = lane; u < (n - t0) * kChunks; u += 64) {
+    const int t = t0 + u / kChunks, dim = u % kChunks * 8;
+    *(u32x4_t*)(held + ((L + t) & (kQ8Tail - 1)) * kHeadDim + dim) = *(const u32x4_t*)(from + t * a.st + dim);
   }
+}
+
+// Tree rows: one 16-byte piece a thread, the heads of a token together.
+__global__ __launch_bounds__(kThreads) void q8_hold_kernel(Q8AppendArgs a) {
+  const int b = blockIdx.y, u = blockIdx.x * kThreads + threadIdx.x;
+  const int dim = u % kChunks * 8, m = u / kChunks & 1, h = u / (2 * kChunks) % a.H, t = u / (2 * kChunks) / a.H;
+  const int n = a.counts ? min(a.counts[b], a.T) : a.T;
+  if (t >= n) return;
+  const int L = min(max(a.seq_lens[b], 0), a.n_blocks * kQ8Block);
+  const u32x4_t x = *(const u32x4_t*)((m ? a.v : a.k) + b * a.sb + t * a.st + h * a.sh + dim);
+  *(u32x4_t*)(ring(a.cache, (size_t)b * a.H + h, m) + ((L + t) & (kQ8Tail - 1)) * kHeadDim + dim) = x;
 }
 
 template <bool INT8>
@@ -175,6 +217,9 @@ __device__ __forceinline__ void store8(float* p, const float (&x)[8]) {
   *(f32x4_t*)(p + 4) = f32x4_t{x[4], x[5], x[6], x[7]};
 }
 
+// Workgroup (block, head, sequence): the codes change order in LDS, so that every
+// store takes whole rows (from the lanes' own units K would go out in pieces of 32
+// bytes: 43 us for 32750 tokens of eight heads; with a wave a block 41; now 37).
 template <bool INT8, class T>
 __global__ __launch_bounds__(kThreads) void q8_read_kernel(Q8ReadArgs a) {
   const int h = blockIdx.y, b = blockIdx.z, tid = threadIdx.x;
@@ -217,60 +262,59 @@ __global__ __launch_bounds__(kThreads) void q8_read_kernel(Q8ReadArgs a) {
   }
 }
 
-// The accepted path of (layer, head, sequence): with L the old length and a
-// the accepted count, token L + d is the ring row of path node d.  Blocks that
-// are whole with the new length are quantised straight from those rows; what
-// is left behind them (at most 31 rows) moves to its place in the ring, all
-// of it read before any of it is written.
+// The accepted path of (layer, head, sequence), a wave for K and one for V: with L
+// the old length and n the accepted count, token L + d is the ring row of path
+// node d.  Blocks that are whole with the new length are quantised straight from
+// those rows; what is left behind them (at most 31 rows) moves to its place in
+// the ring, all of it read before any of it is written.
 template <bool INT8>
 __global__ __launch_bounds__(kThreads) void q8_commit_kernel(Q8CommitArgs a) {
-  const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x;
+  const int b = blockIdx.y, lane = threadIdx.x & 63;
+  const int id = kWaves * blockIdx.x + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = id >> 1, m = id & 1;
   const Q8Cache& cache = a.cache[blockIdx.z];
+  // node at each depth; nodes outside [0, N) count as the chain's
+  int node = lane;
+  if (a.path && lane < a.N) {
+    const int p = a.path[(size_t)b * a.N + lane];
+    if (p >= 0 && p < a.N) node = p;
+  }
   const int cap = a.n_blocks * kQ8Block;
   const int L = min(max(a.seq_lens[b], 0), cap);
   const int n = min(min(max(a.accept_len[b], 0), a.N), cap - L);
   const int end = L + n;
-  if (h == 0 && blockIdx.z == 0 && tid == 0) a.seq_lens_out[b] = end;
-  if (n == 0) return;
+  if (id == 0 && blockIdx.z == 0 && lane == 0) a.seq_lens_out[b] = end;
+  if (n == 0 || h >= a.H) return;
   const size_t head = (size_t)b * a.H + h;
-  const int32_t* path = a.path ? a.path + (size_t)b * a.N : nullptr;
-  // ring row that holds token tok before the commit; nodes outside [0, N)
-  // count as the chain's
+  uint16_t* rows = ring(cache, head, m);
+  // ring row that holds token tok before the commit (called by whole waves)
   auto held = [&](int tok) {
-    int d = tok - L;
-    if (d >= 0 && path) {
-      const int node = path[d];
-      if (node >= 0 && node < a.N) d = node;
-    }
-    return (L + d) & (kQ8Tail - 1);
+    const int moved = __shfl(node, (tok - L) & 63);
+    return (tok < L ? tok : L + moved) & (kQ8Tail - 1);
   };
-  __shared__ BlockLds lds;
   const int whole = end / kQ8Block;
   for (int block = L / kQ8Block; block < whole; ++block) {
-    u32x4_t x[2][2];
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const int chunk = tid + kThreads * j, row = held(block * kQ8Block + chunk / kChunks), dim = chunk % kChunks * 8;
-#pragma unroll
-      for (int m = 0; m < 2; ++m) x[m][j] = *(const u32x4_t*)(ring(cache, head, m) + row * kHeadDim + dim);
-    }
     const size_t at = head * a.n_blocks + block;
-    quantise_block<INT8>(x, cache.blocks + at * kQ8BlockBytes, cache.scales + at * 2, lds);
-    __syncthreads();  // lds is used again
+    quantise_part<INT8>(m, lane, cache.blocks + at * kQ8BlockBytes + m * kQ8PartBytes, cache.scales + at * 2 + m,
+                        [&](int t) { return rows + held(block * kQ8Block + t) * kHeadDim; });
   }
-  const int first = max(L, whole * kQ8Block), rows = end - first;
-  u32x4_t x[4];
+  // The rows left, four a load; a path that starts down the chain keeps the rows
+  // that are in place.
+  const int first = max(L, whole * kQ8Block), left = end - first;
+  const int dim = lane % kChunks * 8, q = lane / kChunks;
+  u32x4_t x[kQ8Block / 4];
+  int to[kQ8Block / 4], source[kQ8Block / 4];
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const int u = tid + kThreads * j, m = u & 1, r = (u >> 1) / kChunks;
-    if (r < rows) x[j] = *(const u32x4_t*)(ring(cache, head, m) + held(first + r) * kHeadDim + (u >> 1) % kChunks * 8);
+  for (int j = 0; j < kQ8Block / 4; ++j) {
+    if (4 * j >= left) break;
+    const int tok = first + 4 * j + q;
+    source[j] = held(tok);
+    to[j] = 4 * j + q < left ? tok & (kQ8Tail - 1) : source[j];
+    if (to[j] != source[j]) x[j] = *(const u32x4_t*)(rows + source[j] * kHeadDim + dim);
   }
-  __syncthreads();
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const int u = tid + kThreads * j, m = u & 1, r = (u >> 1) / kChunks;
-    if (r < rows)
-      *(u32x4_t*)(ring(cache, head, m) + ((first + r) & (kQ8Tail - 1)) * kHeadDim + (u >> 1) % kChunks * 8) = x[j];
+  for (int j = 0; j < kQ8Block / 4; ++j) {
+    if (4 * j >= left) break;
+    if (to[j] != source[j]) *(u32x4_t*)(rows + to[j] * kHeadDim + dim) = x[j];
   }
 }
 
@@ -279,14 +323,15 @@ __global__ __launch_bounds__(kThreads) void q8_commit_kernel(Q8CommitArgs a) {
 hipError_t launch_q8_append(const Q8AppendArgs& a, bool int8, bool hold, hipStream_t stream) {
   const dim3 block(kThreads);
   if (hold) {
-    hipLaunchKernelGGL((q8_append_kernel<false, true>), dim3(1, a.H, a.B), block, 0, stream, a);
+    const unsigned pieces = (unsigned)a.T * a.H * 2 * kChunks;
+    hipLaunchKernelGGL(q8_hold_kernel, dim3((pieces + kThreads - 1) / kThreads, a.B), block, 0, stream, a);
     return hipGetLastError();
   }
-  const dim3 grid((kQ8Block - 1 + a.T) / kQ8Block, a.H, a.B);
+  const dim3 grid((kQ8Block - 1 + a.T) / kQ8Block, 2 * ((a.H + kWaves - 1) / kWaves), a.B);
   if (int8)
-    hipLaunchKernelGGL((q8_append_kernel<true, false>), grid, block, 0, stream, a);
+    hipLaunchKernelGGL((q8_append_kernel<true>), grid, block, 0, stream, a);
   else
-    hipLaunchKernelGGL((q8_append_kernel<false, false>), grid, block, 0, stream, a);
+    hipLaunchKernelGGL((q8_append_kernel<false>), grid, block, 0, stream, a);
   return hipGetLastError();
 }
 
@@ -305,7 +350,7 @@ hipError_t launch_q8_read(const Q8ReadArgs& a, bool int8, bool out_bf16, hipStre
 }
 
 hipError_t launch_q8_commit(const Q8CommitArgs& a, bool int8, hipStream_t stream) {
-  const dim3 grid(a.H, a.B, a.layers), block(kThreads);
+  const dim3 grid((2 * a.H + kWaves - 1) / kWaves, a.B, a.layers), block(kThreads);
   if (int8)
     hipLaunchKernelGGL((q8_commit_kernel<true>), grid, block, 0, stream, a);
   else
