@@ -654,6 +654,8 @@ int glide_q8_tree_attn(const void* q, const glide_q8_cache* cache, const int32_t
   a.splits = p.splits;
   a.target = p.target;
   a.min_units = p.min_units;
+  a.whole_units = p.whole_units;
+  a.long_run = p.long_run;
   a.runs = (int)p.runs;
   const double sc = scale > 0.f ? (double)scale : 1.0 / sqrt((double)D);
   a.scale_log2 = (float)(sc * 1.4426950408889634);  // log2(e)

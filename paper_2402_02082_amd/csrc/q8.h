@@ -79,10 +79,11 @@ hipError_t launch_q8_commit(const Q8CommitArgs& a, bool int8, hipStream_t stream
 // How the attention over an 8-bit cache is divided: workgroups of `waves` waves
 // for `rows` query rows, `groups` of them over the rows of a cached head, and its
 // keys in runs of units -- `splits` of every pair (sequence, cached head), or
-// with splits == 0 up to `target` of equal size in all, of at least min_units
-// units each.  runs: at most so many.
+// with splits == 0 up to `target` (half of it if they would be shorter than
+// long_run units then) of about equal size in all, of at least min_units units
+// each, and pairs of up to whole_units in one.  runs: at most so many.
 struct Q8AttnPlan {
-  int rows, groups, waves, splits, target, min_units;
+  int rows, groups, waves, splits, target, min_units, whole_units, long_run;
   long runs;
   size_t ws_bytes, part_ml_off, part_o_off;
 };
@@ -97,7 +98,7 @@ struct Q8AttnArgs {
   unsigned* counters;  // arrival counters of pairs that lie in several runs
   float* part_o;    // [runs, groups, rows, D]: normalised outputs
   float2* part_ml;  // [runs, groups, rows]: (max in log2 units, sum)
-  int B, N, H, H_kv, n_blocks, groups, splits, target, min_units, runs;
+  int B, N, H, H_kv, n_blocks, groups, splits, target, min_units, whole_units, long_run, runs;
   float scale_log2;
 };
 hipError_t launch_q8_attn(const Q8AttnArgs& a, bool int8, int rows, int waves, hipStream_t stream);

@@ -139,11 +139,6 @@ __device__ __forceinline__ uint64_t ancestor_mask(int p, int lane) {
   return ((uint64_t)hi << 32) | lo;
 }
 
-constexpr int kWholeUnits = 24;  // a pair of so few units is not split: joining would cost more than it saves
-// Up to one run a CU, but two from so many units a run on (7B layer of 2048
-// tokens: 8 runs a pair 10.4 us, 9 14.4; one head group of 60000 tokens, 32 runs a
-// pair 25.7, 63 28.2; 128 pairs of 160 units 36.8 with one, 35.0 with two).
-constexpr int kLongRun = 32;
 constexpr int kRingCost = 4;  // blocks that take a wave about as long as a unit of ring rows
 
 constexpr float kRescaleSlack = 8.f;  // how far a score may pass the reference maximum (log2)
@@ -290,7 +285,7 @@ struct Run {
 
 // Runs of a pair of so many units, of up to `per` units each.
 __device__ __forceinline__ int runs_of(const Q8AttnArgs& a, int units, int per) {
-  return a.splits ? a.splits : (units <= kWholeUnits ? 1 : (units + per - 1) / per);
+  return a.splits ? a.splits : (units <= a.whole_units ? 1 : (units + per - 1) / per);
 }
 
 // Units of sequence b, 0 past the last; `mine`: of the lane's among the first 64.
@@ -329,14 +324,14 @@ __device__ __forceinline__ bool find_run(const Q8AttnArgs& a, bool tree, int run
     }
   } else if (a.B == 1) {
     const int units = sequence(a, tree, 0).units;
-    const int most = units * a.H_kv >= a.target * kLongRun ? a.target : (a.target + 1) / 2, n = max(1, most / a.H_kv);
+    const int most = units * a.H_kv >= a.target * a.long_run ? a.target : (a.target + 1) / 2, n = max(1, most / a.H_kv);
     per = max((units + n - 1) / n, a.min_units);
   } else {
-    // about the fewest units a run with which no more than `most` runs come out:
+    // about the fewest units a run with which no more than `most` runs come out;
     // n pairs of any lengths have about n / 2 runs more than whole ones would be
     const int mine = lane < a.B ? sequence(a, tree, lane).units : 0;
     const int total = sum_of(a, tree, 0, lane, mine) * a.H_kv;
-    const int most = total >= a.target * kLongRun ? a.target : (a.target + 1) / 2;
+    const int most = total >= a.target * a.long_run ? a.target : (a.target + 1) / 2;
     const int whole = max(1, most - a.B * a.H_kv / 2);
     per = max((total + whole - 1) / whole, a.min_units);
     for (int i = 0; i < 16 && sum_of(a, tree, per, lane, mine) * a.H_kv > most; ++i) per += (per + 7) / 8;
@@ -823,13 +818,6 @@ hipError_t launch_rows(const Q8AttnArgs& a, bool int8, hipStream_t stream) {
 
 }  // namespace
 
-// Pairs up to which pairs are split.  The eight waves of a pair on half of the
-// CUs draw the whole memory bandwidth, and joining splits takes 3 us (13B layer,
-// 160 pairs: one run a pair 28 us, two 35 us); 128 pairs of unequal length are
-// faster in up to 512 runs of four waves (46 against 37 us).
-constexpr int kMostSplit = kNumCU / 2;
-constexpr int kMinUnits = 8;  // units of a run at least, of pairs that are split
-
 Q8AttnPlan plan_q8_attn(int B, int N, int H, int H_kv, int n_blocks, int max_splits) {
   Q8AttnPlan p{};
   const int R = N * (H / H_kv);
@@ -837,22 +825,31 @@ Q8AttnPlan plan_q8_attn(int B, int N, int H, int H_kv, int n_blocks, int max_spl
   p.groups = (R + p.rows - 1) / p.rows;
   p.waves = 8;
   const long pairs = (long)B * H_kv, most = n_blocks + (kQ8Block - 1 + N + kQ8Block - 1) / kQ8Block;
-  // (pairs past the counters are not split either way)
-  if (max_splits == 1 || most == 1 || pairs * p.groups > (max_splits ? kCounterSlots : kMostSplit)) {
+  const long wgs = pairs * p.groups;  // one a pair and group
+  // Enough for every CU: nothing is split (nor past the counters).
+  if (max_splits == 1 || most == 1 || wgs > (max_splits ? kCounterSlots : kNumCU - 1)) {
     p.splits = 1;
     p.runs = pairs;
     return p;
   }
-  // 64 rows take eight waves, one workgroup a CU; fewer rows four waves, two
-  if (p.rows < 64) p.waves = 4;
+  const bool few = wgs <= kNumCU / 2;
+  // 64 rows take eight waves, one workgroup a CU; fewer rows of few pairs four waves, two.
+  if (p.rows < 64 && few) p.waves = 4;
   if (max_splits > 0) {
     p.splits = (int)min((long)max_splits, most);
     p.runs = pairs * p.splits;
   } else {
-    p.min_units = kMinUnits;
-    p.target = max(1, 2 * kNumCU / p.groups);
-    p.runs = max(pairs, min(pairs + p.target, pairs * ((most + kMinUnits - 1) / kMinUnits)));
-    if (most <= kWholeUnits) return p;  // no pair will be split: no states
+    // Joining runs takes 3 us, so short pairs are not split, and where workgroups
+    // take more than half of the CUs only those that are long for their call are.
+    p.whole_units = few ? 24 : 48;
+    p.min_units = few ? 8 : 16;
+    // Up to one run a CU; of few pairs two from 32 units a run on (7B layer of 2048
+    // tokens: 8 runs a pair 10.4 us, 9 14.4; one head group of 60000 tokens, 32
+    // runs a pair 25.7, 63 28.2; 128 pairs of 160 units 36.8 with one, 35.0 with two).
+    p.target = max(1, (few ? 2 : 1) * kNumCU / p.groups);
+    p.long_run = few ? 32 : 0;
+    p.runs = max(pairs, min(pairs + p.target, pairs * ((most + p.min_units - 1) / p.min_units)));
+    if (most <= p.whole_units) return p;  // no pair will be split: no states
   }
   const size_t states = (size_t)p.runs * p.groups * p.rows;
   p.part_ml_off = kCounterBytes;
