@@ -450,7 +450,7 @@ typedef struct glide_rope_rows {
  *             must be NULL); else seq_lens[b] (0 without) plus t, or plus the
  *             number of node t's ancestors if tree_parents [B, T] is given:
  *             the positions of a tree behind a prefix of seq_lens[b] tokens.
- *   D == 128; 2 <= rot_dim <= D, even; T >= 1 (tree: <= 64);
+ *   D == 128; 2 <= rot_dim <= D, even; 1 <= T <= 4194304 (tree: <= 64);
  *   1 <= B <= 65535; H >= 1; B * T * (q->H + k->H) < 2^31;
  *   dtype     GLIDE_BF16 or GLIDE_F32 (rows; arithmetic in float32, the angle
  *             reduced in float64).
@@ -524,8 +524,9 @@ typedef struct glide_q8_cache {
  *     multiples of 8; 16-byte aligned).
  *   seq_lens [B] int32, clamped to [0, L_cap]; counts [B] int32 or NULL: rows of
  *     each sequence that are written (clamped to [0, T]; NULL: T).
- *   D == 128; B, H_kv <= 65535; 1 <= T; 32 <= L_cap <= 4194304, a multiple of 32;
- *   kind GLIDE_E4M3 or GLIDE_INT8.
+ *   D == 128; B, H_kv <= 65535, B * H_kv <= 2^21; 1 <= T <= 4194304;
+ *   32 <= L_cap <= 4194304, a multiple of 32; kind GLIDE_E4M3 or GLIDE_INT8 (so
+ *   for every call on an 8-bit cache).
  */
 int glide_q8_append(const void* k_new, const void* v_new, int64_t stride_b, int64_t stride_t,
                     int64_t stride_h, const int32_t* seq_lens, const int32_t* counts, int hold,
@@ -547,14 +548,15 @@ int glide_q8_read(const glide_q8_cache* cache, const int32_t* seq_lens, void* k_
  * glide_q8_tree_attn -- glide_tree_attn over an 8-bit cache: the query rows of
  * sequence b see its tokens [0, seq_lens[b]) and, in tree mode, the tail rows of
  * the nodes that are their own or an ancestor's (held by glide_q8_append).
- *   q, out       [B, N, H, D] bfloat16, 16-byte aligned; H a multiple of H_kv:
- *                query heads j * H / H_kv .. read cached head j.
+ *   q, out       [B, N, H, D] bfloat16, 16-byte aligned, apart; H a multiple of
+ *                H_kv: query heads j * H / H_kv .. read cached head j.
  *   seq_lens     [B] int32, clamped to [0, L_cap].
  *   tree_parents [B, N] int32, or NULL (cross mode).
  *   scale, max_splits, workspace: as glide_tree_attn (the workspace begins with
  *                the same block of arrival counters, zero before its first use
  *                and left zero by every call: one buffer can serve both).
- *   1 <= N <= 64; B <= 65535; B * N * H < 2^31; D == 128.
+ *   1 <= N <= 64; B * N * H < 2^28.  One launch; results do not depend on
+ *   which workgroup runs when.
  * Precision: scores, sums and outputs accumulate in float32 from exact codes;
  * probabilities enter the PV product with 11 significant bits (those below
  * 2^-21 of a row's largest with fewer).  Tree rows that are not finite reach
@@ -577,7 +579,7 @@ int glide_q8_tree_attn(const void* q, const glide_q8_cache* cache, const int32_t
  *              glide_verify_commit gives it (with layers == 0 there), or NULL:
  *              the nodes are a chain, 0, 1, ... (spec_sample_verify).
  *   seq_lens_out [B] int32 out (must not be seq_lens).
- *   1 <= N <= 64; B, H_kv <= 65535; D == 128.  One launch.
+ *   1 <= N <= 64.  One launch.
  */
 int glide_q8_commit(const glide_q8_cache* caches, int layers, const int32_t* seq_lens,
                     const int32_t* accept_len, const int32_t* path, int32_t* seq_lens_out, int B,

@@ -168,6 +168,7 @@ static_assert(GLIDE_Q8_BLOCK == glide::kQ8Block && GLIDE_Q8_TAIL == glide::kQ8Ta
 
 bool q8_sizes_ok(int B, int H_kv, int D, int L_cap, int kind) {
   if (B < 1 || B > 65535 || H_kv < 1 || H_kv > 65535 || D != glide::kHeadDim) return false;  // grid dims
+  if ((double)B * H_kv > (1 << 21)) return false;  // 128 GiB of tails alone
   if (L_cap < glide::kQ8Block || L_cap > kMaxKeys || L_cap % glide::kQ8Block) return false;
   return kind == GLIDE_E4M3 || kind == GLIDE_INT8;
 }
@@ -196,7 +197,8 @@ int q8_lens_check(const int32_t* seq_lens, const int32_t* more, int fixed, int m
 bool q8_attn_sizes_ok(int B, int N, int H, int H_kv, int D, int L_cap) {
   if (!q8_sizes_ok(B, H_kv, D, L_cap, GLIDE_E4M3)) return false;
   if (N < 1 || N > glide::kMaxNodes || H < H_kv || H % H_kv) return false;
-  return (double)B * N * H <= 2147483647.0;
+  // with that, at most 2^21 + 2^22 workgroups of 512 threads: a grid's 2^32
+  return (double)B * N * H < (1 << 28);
 }
 
 bool rope_rows_ok(const glide_rope_rows* r, int B, int T, int elem) {
@@ -502,7 +504,7 @@ int glide_rope(const glide_rope_rows* q, const glide_rope_rows* k, const double*
                hipStream_t stream) {
   if (!q || !freqs || (dtype != GLIDE_BF16 && dtype != GLIDE_F32)) return GLIDE_EINVAL;
   const int elem = dtype == GLIDE_BF16 ? 2 : 4;
-  if (B < 1 || B > 65535 || T < 1 || D != glide::kHeadDim) return GLIDE_EINVAL;
+  if (B < 1 || B > 65535 || T < 1 || T > kMaxKeys || D != glide::kHeadDim) return GLIDE_EINVAL;  // grid dims
   if (!rope_rows_ok(q, B, T, elem) || (k && !rope_rows_ok(k, B, T, elem))) return GLIDE_EINVAL;
   if (rot_dim < 2 || rot_dim > D || rot_dim % 2 || !isfinite(mscale)) return GLIDE_EINVAL;
   if (flags & ~(GLIDE_ROPE_INTERLEAVED | GLIDE_ROPE_BACKWARD)) return GLIDE_EINVAL;
@@ -639,7 +641,6 @@ int glide_q8_tree_attn(const void* q, const glide_q8_cache* cache, const int32_t
   a.seq_lens = seq_lens;
   a.parents = tree_parents;
   a.out = (uint16_t*)out;
-  if (p.runs * p.groups > 2147483640L) return GLIDE_EINVAL;  // a grid dimension
   if (p.ws_bytes > 0) {
     a.counters = (unsigned*)workspace;
     a.part_ml = (float2*)((char*)workspace + p.part_ml_off);

@@ -28,7 +28,7 @@ def _cache(blocks=FAKE, scales=FAKE, tail=FAKE):
 BAD_CACHES = [dict(blocks=None), dict(scales=None), dict(tail=None), dict(blocks=FAKE + 8), dict(scales=FAKE + 4),
               dict(tail=FAKE + 2)]
 BAD_SIZES = [dict(B=0), dict(B=65536), dict(Hkv=0), dict(Hkv=65536), dict(D=64), dict(L_cap=0), dict(L_cap=16),
-             dict(L_cap=100), dict(L_cap=(1 << 22) + 32), dict(kind=0), dict(kind=1), dict(kind=4)]
+             dict(L_cap=100), dict(L_cap=(1 << 22) + 32), dict(B=1 << 15, Hkv=128), dict(kind=0), dict(kind=1), dict(kind=4)]
 
 
 def _rope(lib, **kw):
@@ -47,7 +47,7 @@ def _rope(lib, **kw):
     dict(qs=(0, 4100, 128)), dict(qos=(0, 4096, 130)), dict(ks=(-8, 1024, 128)), dict(qs=(0, 4096, 2), dtype=1),
     dict(H=0), dict(Hkv=0), dict(rot=0), dict(rot=3), dict(rot=130), dict(m=float("nan")), dict(m=float("inf")),
     dict(pos=FAKE), dict(pos=FAKE, lens=None), dict(pos=FAKE, par=None), dict(B=0), dict(B=65536), dict(T=0),
-    dict(T=65), dict(D=64), dict(dtype=2), dict(dtype=-1), dict(flags=4), dict(par=None, T=1 << 21, B=64),
+    dict(T=65), dict(par=None, T=(1 << 22) + 1), dict(D=64), dict(dtype=2), dict(dtype=-1), dict(flags=4), dict(par=None, T=1 << 21, B=64),
 ])
 def test_rope_rejects(lib, bad):
     assert _rope(lib, **bad) == EINVAL
@@ -140,7 +140,7 @@ def _attn(lib, cache=None, **kw):
 
 @pytest.mark.parametrize("bad", BAD_SIZES + [
     dict(q=None), dict(lens=None), dict(out=None), dict(q=FAKE + 2), dict(out=FAKE + 8), dict(N=0), dict(N=65),
-    dict(H=0), dict(H=4), dict(H=12), dict(B=65535, N=64, H=1024), dict(scale=float("nan")),
+    dict(H=0), dict(H=4), dict(H=12), dict(B=4096, N=64, H=1024, Hkv=1), dict(scale=float("nan")),
     dict(scale=float("inf")), dict(splits=-1), dict(splits=65), dict(ws=None), dict(ws_bytes=16), dict(ws=FAKE + 4)])
 def test_attn_rejects(lib, bad):
     assert _attn(lib, **bad) == EINVAL

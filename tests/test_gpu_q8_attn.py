@@ -38,7 +38,7 @@ def fill(B, H, lens, kind, seed, cap=None, k_scale=1.0, v_scale=1.0):
     return cache, k, v
 
 
-def check(got, q, k, v, lens, kind, tk=None, tv=None, par=None, scale=None, nodes=None):
+def check(got, q, k, v, lens, kind, tk=None, tv=None, par=None, scale=None, nodes=None, pairs=None):
     got, q = f64(got), f64(q)
     B, N, H, D = q.shape
     Hk = k.shape[2]
@@ -46,6 +46,8 @@ def check(got, q, k, v, lens, kind, tk=None, tv=None, par=None, scale=None, node
     sc = 1 / np.sqrt(D) if scale is None else scale
     for b in range(B):
         for j in range(Hk):
+            if pairs is not None and (b, j) not in pairs:
+                continue
             ks, vs = (OQ.stored(f64(x[b, :lens[b], j]), kind) for x in (k, v))
             for n in range(N) if nodes is None else nodes:
                 kk, vv = ks, vs
@@ -136,6 +138,35 @@ def test_one_sequence_and_many_rows(kind):
         par = [random_tree(N, np.random.default_rng(N))]
         q = cpu_normal((1, N, H, 128), 17, BF).cuda()
         check(run(q, cache, lens, par), q, k, v, lens, kind, tk, tv, par, nodes=sorted({0, N // 2, N - 1}))
+
+
+@pytest.mark.parametrize("B,H,Hk,N,top", [
+    (2, 4, 2, 5, 3000), (3, 16, 4, 30, 1500), (5, 64, 8, 9, 2100), (4, 40, 40, 7, 3500), (9, 20, 20, 33, 1900),
+    (6, 32, 32, 1, 2600), (3, 80, 20, 25, 1800), (70, 8, 4, 3, 500), (70, 6, 6, 2, 300), (130, 1, 1, 6, 1800)])
+def test_plans(B, H, Hk, N, top):
+    """Few pairs, as many as half of the CUs, more, as many as all and more; up to
+    64 sequences and beyond; several groups of query rows: unequal lengths, some
+    of one token; some pairs against the oracle, all against one run a pair (each
+    is within a rounding to bfloat16, 2^-8 of it, and 2^-10 of the largest value
+    from the exact result), and two calls alike."""
+    require_gpu()
+    say("plans", B, H, Hk, N, top)
+    rng = np.random.default_rng(B + N)
+    lens = [int(x) for x in rng.integers(1, top, B)]
+    lens[0], lens[-1] = top, 1
+    cache, k, v = fill(B, Hk, lens, "int8", 50)
+    tk, tv = rows((B, N, Hk, 128), 51), rows((B, N, Hk, 128), 52)
+    glide.glide_q8_append(tk, tv, cache, ints(lens), hold=True)
+    q = cpu_normal((B, N, H, 128), 53, BF).cuda()
+    for par in (None, [random_tree(N, rng) for _ in range(B)]):
+        out = run(q, cache, lens, par)
+        pairs = {(0, 0), (B - 1, Hk - 1), (B // 2, Hk // 2)}
+        check(out, q, k, v, lens, "int8", *((tk, tv, par) if par else ()), nodes=sorted({0, N - 1}), pairs=pairs)
+        one = run(q, cache, lens, par, max_splits=1)
+        size = float(v.abs().max().float())
+        err = (out.float() - one.float()).abs()
+        assert bool((err <= 2.0 ** -7 * one.float().abs() + 2.0 ** -9 * size).all())
+        assert torch.equal(run(q, cache, lens, par), out)
 
 
 @pytest.mark.parametrize("kind", KINDS)
