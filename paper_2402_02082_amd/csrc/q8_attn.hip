@@ -502,6 +502,24 @@ void q8_attn_kernel(Q8AttnArgs a) {
   const int G = a.H / a.H_kv, R = a.N * G, row0 = grp * kRows + rg * 16 * NT;
   __shared__ JoinLds<WAVES, 16 * NT> lds;
 
+  // Query rows: row r is node r / G of query head hk * G + r % G.  MFMA step
+  // 2 h + e holds dims 64 h + 16 g + 8 e + (0..7).  A single sequence's are
+  // requested before its length is known.
+  int node[NT];
+  u32x4_t qf[NT][4];
+  auto load_queries = [&](int b, int hk) {
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      const int r = row0 + 16 * nt + c;
+      node[nt] = r < R ? r / G : 0;
+      const uint16_t* q = a.q + (((size_t)b * a.N + node[nt]) * a.H + hk * G + (r - node[nt] * G)) * kD;
+#pragma unroll
+      for (int st = 0; st < 4; ++st)
+        qf[nt][st] = r < R ? *(const u32x4_t*)(q + 64 * (st >> 1) + 16 * g + 8 * (st & 1)) : u32x4_t{0, 0, 0, 0};
+    }
+  };
+  if (a.B == 1) load_queries(0, run % a.H_kv);
+
   Run rn;
   if (!find_run(a, TREE, run, lane, &rn)) return;
   const int b = rn.b, hk = rn.hk, u0 = rn.u0, u1 = rn.u1;
@@ -537,19 +555,7 @@ void q8_attn_kernel(Q8AttnArgs a) {
       load_v<kPolicy>(raw[i], r, lane);
     }
   };
-  // Query rows: row r is node r / G of query head hk * G + r % G.  MFMA step
-  // 2 h + e holds dims 64 h + 16 g + 8 e + (0..7).
-  int node[NT];
-  u32x4_t qf[NT][4];
-#pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
-    const int r = row0 + 16 * nt + c;
-    node[nt] = r < R ? r / G : 0;
-    const uint16_t* q = a.q + (((size_t)b * a.N + node[nt]) * a.H + hk * G + (r - node[nt] * G)) * kD;
-#pragma unroll
-    for (int st = 0; st < 4; ++st)
-      qf[nt][st] = r < R ? *(const u32x4_t*)(q + 64 * (st >> 1) + 16 * g + 8 * (st & 1)) : u32x4_t{0, 0, 0, 0};
-  }
+  if (a.B > 1) load_queries(b, hk);
 
   // The first blocks are requested now, unless the wave has ring rows and no
   // registers to hold the blocks through their scores.
