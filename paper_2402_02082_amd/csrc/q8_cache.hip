@@ -206,22 +206,22 @@ __device__ __forceinline__ float value_of(uint8_t code) {
   return INT8 ? (float)((int)code - 128) : __builtin_amdgcn_cvt_f32_fp8((int)code, 0);
 }
 
-__device__ __forceinline__ void store8(uint16_t* p, const float (&x)[8]) {
+// A 16-byte piece of an output row.
+__device__ __forceinline__ void store_piece(uint16_t* p, const float (&x)[8]) {
   u32x4_t w;
 #pragma unroll
   for (int e = 0; e < 4; ++e) w[e] = pack_bf16x2(x[2 * e], x[2 * e + 1]);
   *(u32x4_t*)p = w;
 }
-__device__ __forceinline__ void store8(float* p, const float (&x)[8]) {
-  *(f32x4_t*)p = f32x4_t{x[0], x[1], x[2], x[3]};
-  *(f32x4_t*)(p + 4) = f32x4_t{x[4], x[5], x[6], x[7]};
-}
+__device__ __forceinline__ void store_piece(float* p, const float (&x)[4]) { *(f32x4_t*)p = f32x4_t{x[0], x[1], x[2], x[3]}; }
 
 // Workgroup (block, head, sequence): the codes change order in LDS, so that every
 // store takes whole rows (from the lanes' own units K would go out in pieces of 32
-// bytes: 43 us for 32750 tokens of eight heads; with a wave a block 41; now 37).
+// bytes: 43 us for 32750 tokens of eight heads; with a wave a block 41; now 37,
+// 201 MB at 5.4 TB/s).
 template <bool INT8, class T>
 __global__ __launch_bounds__(kThreads) void q8_read_kernel(Q8ReadArgs a) {
+  constexpr int V = 16 / sizeof(T), kPieces = kHeadDim / V;  // dims of a piece, pieces of a row
   const int h = blockIdx.y, b = blockIdx.z, tid = threadIdx.x;
   const int block = a.start / kQ8Block + blockIdx.x;
   const int L = min(max(a.seq_lens[b], 0), a.n_blocks * kQ8Block);
@@ -240,25 +240,26 @@ __global__ __launch_bounds__(kThreads) void q8_read_kernel(Q8ReadArgs a) {
           *(const u32x4_t*)(a.cache.blocks + at * kQ8BlockBytes + m * kQ8PartBytes + tid * 16);
   }
   __syncthreads();
+  constexpr int kTurns = kQ8Block * kPieces / kThreads;  // of K, and of V
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const int m = j >> 1, chunk = tid + kThreads * (j & 1), row = chunk / kChunks, dim = chunk % kChunks * 8;
+  for (int j = 0; j < 2 * kTurns; ++j) {
+    const int m = j / kTurns, piece = tid + kThreads * (j % kTurns), row = piece / kPieces, dim = piece % kPieces * V;
     const int tok = first + row;
     if (tok < a.start || tok >= a.start + a.T || tok >= L) continue;
-    float x[8];
+    float x[V];
     if (whole) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e)
+      for (int e = 0; e < V; ++e)
         x[e] = value_of<INT8>(codes[m ? kQ8PartBytes + q8_v_byte(row, dim + e) : q8_k_byte(row, dim + e)]) * s[m];
     } else {
-      const u32x4_t w = *(const u32x4_t*)(ring(a.cache, head, m) + (tok & (kQ8Tail - 1)) * kHeadDim + dim);
+      const uint16_t* w = ring(a.cache, head, m) + (tok & (kQ8Tail - 1)) * kHeadDim + dim;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        x[2 * e] = __uint_as_float(w[e] << 16);
-        x[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
+      for (int e = 0; e < V; e += 2) {
+        const uint32_t two = *(const uint32_t*)(w + e);
+        x[e] = low_half(two), x[e + 1] = high_half(two);
       }
     }
-    store8((T*)(m ? a.v_out : a.k_out) + (head * a.T + (tok - a.start)) * kHeadDim + dim, x);
+    store_piece((T*)(m ? a.v_out : a.k_out) + (head * a.T + (tok - a.start)) * kHeadDim + dim, x);
   }
 }
 

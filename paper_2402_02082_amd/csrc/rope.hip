@@ -11,9 +11,12 @@
 // 2^22 times a frequency of 1 leaves no correct digit of a turn in float32);
 // sine and cosine of what is left are float32.
 //
-// One workgroup takes one token: its first wave computes the token's up to
-// 64 sines and cosines once for all heads while the rows are on their way,
-// then every thread turns 16 dims of a row at a time.
+// One workgroup takes one to four tokens (enough rows for its threads): a wave
+// computes a token's up to 64 sines and cosines once for all heads while the
+// rows are on their way, then every thread turns two 16-byte pieces of a row at a
+// time, which lie side by side across its lanes (two pieces of a lane side by side
+// instead: 37 us).  Bound: the memory's copy rate (four 2048-token sequences of 40
+// heads, 168 MB in 33 us, 5.1 TB/s); a decoding step's few rows take a launch.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -34,8 +37,11 @@ __device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(f, bf16x2_t));
 }
 
-// Eight consecutive elements.
-__device__ __forceinline__ void load8(float (&x)[8], const uint16_t* p) {
+// A 16-byte piece of a row: kPiece<T> elements as float32.
+template <class T>
+constexpr int kPiece = 16 / sizeof(T);
+
+__device__ __forceinline__ void load_piece(float (&x)[8], const uint16_t* p) {
   const u32x4_t w = *(const u32x4_t*)p;
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
@@ -43,24 +49,19 @@ __device__ __forceinline__ void load8(float (&x)[8], const uint16_t* p) {
     x[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
   }
 }
-__device__ __forceinline__ void load8(float (&x)[8], const float* p) {
-  const float4 a = *(const float4*)p, b = *(const float4*)(p + 4);
-  x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
+__device__ __forceinline__ void load_piece(float (&x)[4], const float* p) {
+  const float4 a = *(const float4*)p;
+  x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w;
 }
-__device__ __forceinline__ void store8(uint16_t* p, const float (&x)[8]) {
+__device__ __forceinline__ void store_piece(uint16_t* p, const float (&x)[8]) {
   u32x4_t w;
 #pragma unroll
   for (int e = 0; e < 4; ++e) w[e] = pack_bf16x2(x[2 * e], x[2 * e + 1]);
   *(u32x4_t*)p = w;
 }
-__device__ __forceinline__ void store8(float* p, const float (&x)[8]) {
+__device__ __forceinline__ void store_piece(float* p, const float (&x)[4]) {
   *(float4*)p = make_float4(x[0], x[1], x[2], x[3]);
-  *(float4*)(p + 4) = make_float4(x[4], x[5], x[6], x[7]);
 }
-__device__ __forceinline__ float load1(const uint16_t* p) { return __uint_as_float((uint32_t)*p << 16); }
-__device__ __forceinline__ float load1(const float* p) { return *p; }
-__device__ __forceinline__ void store1(uint16_t* p, float x) { *p = (uint16_t)pack_bf16x2(x, 0.f); }
-__device__ __forceinline__ void store1(float* p, float x) { *p = x; }
 
 // Depth of node t: its ancestors, followed up by one lane (a chain of at most
 // 63 parents; those outside [-1, node) count as -1).
@@ -74,16 +75,94 @@ __device__ __forceinline__ int depth_of(const int32_t* parents, int t) {
   }
 }
 
-// LAYOUT 0: pairs (2i, 2i + 1); 1: (i, i + rot / 2), both at multiples of 8;
-// 2: (i, i + rot / 2) one by one.
+// Two pieces of one row.  LAYOUT
+//   0: pairs (2i, 2i + 1): piece j of either half of the row;
+//   1: pairs (i, i + rot / 2) where the pieces of a pair's two dims are whole
+//      (rot / 2 a multiple of a piece): V pairs from V j on, past rot / 2 two
+//      pieces of copied dims;
+//   2: the same pairs where they are not: pieces as in 0, and each dim finds the
+//      other one of its pair in a copy of the row in LDS (element by element from
+//      memory 120 us for 8192 tokens of 40 heads, now 34).
 template <class T, int LAYOUT>
+struct Item {
+  static constexpr int V = kPiece<T>, kPerRow = kPairs / V;
+  T* out;
+  int d1, d2;
+  float x1[V], x2[V];
+
+  __device__ __forceinline__ void load(const RopeArgs& a, int b, int t, int i) {
+    int h = i / kPerRow;
+    const int j = i % kPerRow * V, half = a.rot / 2;
+    const bool is_k = h >= a.q.H;
+    const RopeRows& r = is_k ? a.k : a.q;
+    if (is_k) h -= a.q.H;
+    const T* in = (const T*)r.in + b * r.in_sb + t * r.in_st + h * r.in_sh;
+    out = (T*)r.out + b * r.out_sb + t * r.out_st + h * r.out_sh;
+    d1 = LAYOUT == 1 && j >= half ? 2 * j : j;
+    d2 = LAYOUT == 1 ? (j < half ? j + half : 2 * j + V) : j + kPairs;
+    load_piece(x1, in + d1);
+    load_piece(x2, in + d2);
+  }
+
+  // `row`: the row's copy in LDS (LAYOUT 2).  Dims past rot are as they were,
+  // infinities among them.
+  __device__ __forceinline__ void turn_and_store(const float2* cs, int rot, float* row) {
+    const int half = rot / 2;
+    if (LAYOUT == 0) {
+#pragma unroll
+      for (int e = 0; e < V; e += 2) {
+        if (d1 + e < rot) turn(x1[e], x1[e + 1], cs[(d1 + e) / 2]);
+        if (d2 + e < rot) turn(x2[e], x2[e + 1], cs[(d2 + e) / 2]);
+      }
+    } else if (LAYOUT == 1) {
+      if (d1 < half)
+#pragma unroll
+        for (int e = 0; e < V; ++e) turn(x1[e], x2[e], cs[d1 + e]);
+    } else {
+#pragma unroll
+      for (int e = 0; e < V; ++e) row[d1 + e] = x1[e], row[d2 + e] = x2[e];
+      __builtin_amdgcn_wave_barrier();  // a row is one wave's
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        x1[e] = turned(x1[e], d1 + e, cs, rot, half, row);
+        x2[e] = turned(x2[e], d2 + e, cs, rot, half, row);
+      }
+      __builtin_amdgcn_wave_barrier();
+    }
+    store_piece(out + d1, x1);
+    store_piece(out + d2, x2);
+  }
+
+  static __device__ __forceinline__ void turn(float& a, float& b, float2 w) {
+    const float x = a;
+    a = x * w.x - b * w.y;
+    b = b * w.x + x * w.y;
+  }
+
+  static __device__ __forceinline__ float turned(float x, int d, const float2* cs, int rot, int half, const float* row) {
+    if (d >= rot) return x;
+    const bool first = d < half;
+    const float2 w = cs[first ? d : d - half];
+    const float y = row[first ? d + half : d - half];
+    return first ? x * w.x - y * w.y : x * w.x + y * w.y;
+  }
+};
+
+template <class T, int LAYOUT, int TOKENS>
 __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a, float sign) {
-  const int t = blockIdx.x, b = blockIdx.y, tid = threadIdx.x;
-  const int half = a.rot / 2;
-  __shared__ float2 cs[kPairs];
-  if (tid < kPairs) {
+  typedef Item<T, LAYOUT> item_t;
+  constexpr int kRowsAtOnce = LAYOUT == 2 ? kThreads / item_t::kPerRow : 1;
+  const int b = blockIdx.y, tid = threadIdx.x;
+  // the threads of a token; their number is a multiple of a wave's 64
+  const int mine = tid / (kThreads / TOKENS), t = blockIdx.x * TOKENS + mine, at = tid % (kThreads / TOKENS);
+  const int items = t < a.T ? (a.q.H + a.k.H) * item_t::kPerRow : 0;
+  __shared__ float2 cs[TOKENS][kPairs];
+  __shared__ float rows[kRowsAtOnce][kHeadDim + 1];
+  item_t item;
+  if (at < items) item.load(a, b, t, at);  // on its way while the angles are formed
+  if (at < kPairs) {
     float c = 1.f, s = 0.f;
-    if (tid < half) {
+    if (at < a.rot / 2 && t < a.T) {
       int pos;
       if (a.positions) {
         pos = a.positions[(size_t)b * a.T + t];
@@ -91,90 +170,41 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a, float sign) 
         pos = a.seq_lens ? a.seq_lens[b] : 0;
         pos += a.parents ? depth_of(a.parents + (size_t)b * a.T, t) : t;
       }
-      const double turns = (double)pos * (a.freqs[tid] * 0.15915494309189533577);  // 1 / (2 pi)
+      const double turns = (double)pos * (a.freqs[at] * 0.15915494309189533577);  // 1 / (2 pi)
       const float left = (float)(turns - rint(turns));
       sincospif(2.f * left, &s, &c);
       c *= a.mscale;
       s *= a.mscale * sign;
     }
-    cs[tid] = make_float2(c, s);
+    cs[mine][at] = make_float2(c, s);
   }
   __syncthreads();
-  // item: 8 pairs of one row
-  const int items = (a.q.H + a.k.H) * (kPairs / 8);
-  for (int i = tid; i < items; i += kThreads) {
-    int h = i / (kPairs / 8);
-    const int p0 = i % (kPairs / 8) * 8;
-    const bool is_k = h >= a.q.H;
-    const RopeRows& r = is_k ? a.k : a.q;
-    if (is_k) h -= a.q.H;
-    const T* in = (const T*)r.in + b * r.in_sb + t * r.in_st + h * r.in_sh;
-    T* out = (T*)r.out + b * r.out_sb + t * r.out_st + h * r.out_sh;
-    float x1[8], x2[8];  // pair p0 + e
-    int d1 = 0, d2 = 0;  // first dims of the two runs of eight
-    if (LAYOUT == 0) {
-      float lo[8], hi[8];
-      d1 = 2 * p0, d2 = d1 + 8;
-      load8(lo, in + d1);
-      load8(hi, in + d2);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        x1[e] = lo[2 * e], x2[e] = lo[2 * e + 1];
-        x1[4 + e] = hi[2 * e], x2[4 + e] = hi[2 * e + 1];
-      }
-    } else if (LAYOUT == 1) {
-      d1 = p0 < half ? p0 : a.rot + 2 * (p0 - half);
-      d2 = p0 < half ? p0 + half : d1 + 8;
-      load8(x1, in + d1);
-      load8(x2, in + d2);
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int p = p0 + e;
-        x1[e] = load1(in + (p < half ? p : 2 * p));
-        x2[e] = load1(in + (p < half ? p + half : 2 * p + 1));
-      }
-    }
-    float y1[8], y2[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const float2 w = cs[p0 + e];
-      const bool turn = p0 + e < half;  // a copied dim may be infinite
-      y1[e] = turn ? x1[e] * w.x - x2[e] * w.y : x1[e];
-      y2[e] = turn ? x2[e] * w.x + x1[e] * w.y : x2[e];
-    }
-    if (LAYOUT == 0) {
-      float lo[8], hi[8];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        lo[2 * e] = y1[e], lo[2 * e + 1] = y2[e];
-        hi[2 * e] = y1[4 + e], hi[2 * e + 1] = y2[4 + e];
-      }
-      store8(out + d1, lo);
-      store8(out + d2, hi);
-    } else if (LAYOUT == 1) {
-      store8(out + d1, y1);
-      store8(out + d2, y2);
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int p = p0 + e;
-        store1(out + (p < half ? p : 2 * p), y1[e]);
-        store1(out + (p < half ? p + half : 2 * p + 1), y2[e]);
-      }
-    }
+  for (int i = at; i < items; i += kThreads / TOKENS) {
+    item.turn_and_store(cs[mine], a.rot, rows[LAYOUT == 2 ? tid / item_t::kPerRow : 0]);
+    if (i + kThreads / TOKENS < items) item.load(a, b, t, i + kThreads / TOKENS);
   }
+}
+
+template <class T, int LAYOUT>
+void launch_layout(const RopeArgs& a, float sign, hipStream_t stream) {
+  const int items = (a.q.H + a.k.H) * Item<T, LAYOUT>::kPerRow;
+  const dim3 block(kThreads);
+  if (items <= kThreads / 4)
+    hipLaunchKernelGGL((rope_kernel<T, LAYOUT, 4>), dim3((a.T + 3) / 4, a.B), block, 0, stream, a, sign);
+  else if (items <= kThreads / 2)
+    hipLaunchKernelGGL((rope_kernel<T, LAYOUT, 2>), dim3((a.T + 1) / 2, a.B), block, 0, stream, a, sign);
+  else
+    hipLaunchKernelGGL((rope_kernel<T, LAYOUT, 1>), dim3(a.T, a.B), block, 0, stream, a, sign);
 }
 
 template <class T>
 hipError_t launch_type(const RopeArgs& a, bool interleaved, float sign, hipStream_t stream) {
-  const dim3 grid(a.T, a.B), block(kThreads);
   if (interleaved)
-    hipLaunchKernelGGL((rope_kernel<T, 0>), grid, block, 0, stream, a, sign);
-  else if (a.rot % 16 == 0)
-    hipLaunchKernelGGL((rope_kernel<T, 1>), grid, block, 0, stream, a, sign);
+    launch_layout<T, 0>(a, sign, stream);
+  else if (a.rot % (2 * kPiece<T>) == 0)
+    launch_layout<T, 1>(a, sign, stream);
   else
-    hipLaunchKernelGGL((rope_kernel<T, 2>), grid, block, 0, stream, a, sign);
+    launch_layout<T, 2>(a, sign, stream);
   return hipGetLastError();
 }
 
