@@ -574,7 +574,7 @@ int glide_q8_tree_attn(const void* q, const glide_q8_cache* cache, const int32_t
  * L + d takes the tail row of path node path[b, d], d < accept_len[b]; blocks
  * that become whole are quantised; seq_lens_out[b] = L + accept_len[b] (rows
  * past L_cap are dropped and not counted).
- *   caches     HOST array of `layers` caches, 1 <= layers <= 128.
+ *   caches     HOST array of `layers` caches, no two the same, 1 <= layers <= 128.
  *   accept_len [B] int32 (clamped to [0, N]); path [B, N] int32 as
  *              glide_verify_commit gives it (with layers == 0 there), or NULL:
  *              the nodes are a chain, 0, 1, ... (spec_sample_verify).

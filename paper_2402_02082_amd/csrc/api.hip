@@ -6,6 +6,7 @@
 #include <stdlib.h>
 #include <string.h>
 
+#include <algorithm>
 #include <mutex>
 #include <vector>
 
@@ -35,7 +36,12 @@ bool validate_enabled() {
 // Copies a small int32 device array to the host (synchronises `stream`).
 bool fetch_ints(const int32_t* dev, size_t n, std::vector<int32_t>& host, hipStream_t stream,
                 int* status) {
-  host.resize(n);
+  try {
+    host.resize(n);
+  } catch (...) {  // no exception leaves a C entry
+    *status = hip_status(hipErrorOutOfMemory);
+    return false;
+  }
   hipError_t e = hipMemcpyAsync(host.data(), dev, n * sizeof(int32_t), hipMemcpyDeviceToHost, stream);
   if (e == hipSuccess) e = hipStreamSynchronize(stream);
   if (e != hipSuccess) {
@@ -670,8 +676,17 @@ int glide_q8_commit(const glide_q8_cache* caches, int layers, const int32_t* seq
   if (!caches || !seq_lens || !accept_len || !seq_lens_out || seq_lens_out == seq_lens) return GLIDE_EINVAL;
   if (layers < 1 || layers > glide::kQ8MaxLayers || N < 1 || N > glide::kMaxNodes) return GLIDE_EINVAL;
   if (!q8_sizes_ok(B, H_kv, D, L_cap, kind)) return GLIDE_EINVAL;
-  for (int l = 0; l < layers; ++l)
+  const void* tails[glide::kQ8MaxLayers];
+  bool sorted = true;
+  for (int l = 0; l < layers; ++l) {
     if (!q8_cache_ok(&caches[l], &a.cache[l])) return GLIDE_EINVAL;
+    tails[l] = caches[l].tail;
+    sorted = sorted && (l == 0 || (uintptr_t)tails[l - 1] < (uintptr_t)tails[l]);
+  }
+  if (!sorted) {  // a layer given twice would be moved twice at once
+    std::sort(tails, tails + layers);
+    if (std::adjacent_find(tails, tails + layers) != tails + layers) return GLIDE_EINVAL;
+  }
   if (validate_enabled()) {
     int status = q8_lens_check(seq_lens, accept_len, 0, N, B, L_cap, stream);
     if (status != GLIDE_OK) return status;

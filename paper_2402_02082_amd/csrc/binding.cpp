@@ -341,11 +341,14 @@ bool optional_there(PyObject* o, at::ScalarType dtype, at::IntArrayRef shape, co
   return *t && is_shape(**t, shape);
 }
 
-// Element strides of a [B, T, H, 128] tensor whose rows are in one piece;
-// dims of size 1 have none.
+// Element strides of a [B, T, H, 128] tensor whose rows are in one piece, at
+// multiples of 16 bytes; dims of size 1 have none.
 bool row_strides(const at::Tensor& t, int64_t* s) {
-  if (t.dim() != 4 || t.size(3) != GLIDE_HEAD_DIM || t.stride(3) != 1) return false;
-  for (int i = 0; i < 3; ++i) s[i] = t.size(i) > 1 ? t.stride(i) : 0;
+  if (t.dim() != 4 || t.size(3) != GLIDE_HEAD_DIM || t.stride(3) != 1 || (uintptr_t)t.data_ptr() % 16) return false;
+  for (int i = 0; i < 3; ++i) {
+    s[i] = t.size(i) > 1 ? t.stride(i) : 0;
+    if (s[i] * t.element_size() % 16) return false;
+  }
   return true;
 }
 

@@ -166,8 +166,8 @@ def _commit(lib, cache=None, **kw):
     a = dict(layers=2, lens=FAKE, acc=FAKE, path=FAKE, out=FAKE + 64, B=1, N=16, Hkv=32, D=128, L_cap=2048,
              kind=glide.GLIDE_INT8)
     a.update(kw)
-    c = (_lib._Q8Pointers * 130)(*[_cache() for _ in range(130)])
-    c[1] = _cache(**(cache or {}))
+    c = (_lib._Q8Pointers * 130)(*[_cache(tail=FAKE + 32 * i) for i in range(130)])
+    c[1] = _cache(**{**dict(tail=FAKE + 32), **(cache or {})})
     return lib.glide_q8_commit(c, a["layers"], a["lens"], a["acc"], a["path"], a["out"], a["B"], a["N"], a["Hkv"],
                                a["D"], a["L_cap"], a["kind"], None)
 
@@ -176,6 +176,11 @@ def _commit(lib, cache=None, **kw):
                                              dict(layers=0), dict(layers=129), dict(N=0), dict(N=65)])
 def test_commit_rejects(lib, bad):
     assert _commit(lib, **bad) == EINVAL
+
+
+def test_commit_rejects_a_layer_given_twice(lib):
+    for layers, same in ((2, dict(tail=FAKE)), (5, dict(tail=FAKE + 3 * 32)), (128, dict(tail=FAKE + 127 * 32))):
+        assert _commit(lib, cache=same, layers=layers) == EINVAL
 
 
 @pytest.mark.parametrize("bad", BAD_CACHES)

@@ -339,7 +339,8 @@ def test_refusals():
         lambda: glide.glide_q8_commit([c], lens, lens, lens, out),
         lambda: glide.glide_q8_commit([c], lens, lens, torch.zeros((2, 65), dtype=I32, device="cuda"), out),
         lambda: glide.glide_q8_commit([c], lens, lens, None, out, nodes=0),
-        lambda: glide.glide_q8_commit([c] * 129, lens, lens, None, out)]
+        lambda: glide.glide_q8_commit([c] * 129, lens, lens, None, out),
+        lambda: glide.glide_q8_commit([c, c], lens, lens, None, out)]
     for i, call in enumerate(calls):
         with pytest.raises((ValueError, glide.GlideError)):
             call()
