@@ -144,7 +144,7 @@ def _bind():
             lib.glide_block_attn)), _raw_stream, _ws_cache)
         native.bind_q8(tuple(ctypes.cast(f, ctypes.c_void_p).value for f in (
             lib.glide_capture_id, lib.glide_rope, lib.glide_q8_append, lib.glide_q8_read,
-            lib.glide_q8_tree_attn_workspace, lib.glide_q8_tree_attn, lib.glide_q8_commit)))
+            lib.glide_q8_tree_attn_workspace, lib.glide_q8_tree_attn, lib.glide_q8_commit)), _q8_ws_cache)
         _native = native
     return _native
 
@@ -849,6 +849,10 @@ def _glide_q8_read(cache, seq_lens, k_out, v_out, start, stream):
     return k_out, v_out
 
 
+# Workspaces of eager calls, apart from _ws_cache: a captured glide_tree_attn
+# goes on using the one that it found there, so no larger call here may replace it.
+_q8_ws_cache = {}
+
 # Workspaces of captured calls: {(device index, stream handle): (capture, byte
 # tensor)}.  A graph's workspace is its own -- allocated and zeroed inside the
 # capture, in the memory that the graph keeps -- so that two graphs, or a graph
@@ -857,8 +861,8 @@ _captured_ws = {}
 
 
 def q8_attn_workspace(B, N, H, H_kv, L_cap, max_splits, device, stream=None):
-    """The kept workspace of glide_q8_tree_attn for the stream (shared with
-    glide_tree_attn), or under a capture that capture's; None if none is needed."""
+    """The kept workspace of glide_q8_tree_attn for the stream, or under a capture
+    that capture's; None if none is needed."""
     need = load().glide_q8_tree_attn_workspace(B, N, H, H_kv, HEAD_DIM, L_cap, max_splits)
     if need == 0:
         return None
@@ -871,9 +875,9 @@ def q8_attn_workspace(B, N, H, H_kv, L_cap, max_splits, device, stream=None):
         if held is None or held[0] != capture or held[1].numel() < need:
             held = _captured_ws[key] = (capture, _alloc_bytes(need, device, s, zero=True))
         return held[1]
-    ws = _ws_cache.get(key)
+    ws = _q8_ws_cache.get(key)
     if ws is None or ws.numel() < need:
-        ws = _ws_cache[key] = _alloc_bytes(need, device, s, zero=True)
+        ws = _q8_ws_cache[key] = _alloc_bytes(need, device, s, zero=True)
     return ws
 
 

@@ -47,6 +47,7 @@ struct Q8Calls {
 } q8;
 PyObject* raw_stream;  // device index -> current stream handle
 PyObject* workspaces;  // {(device index, stream handle): byte tensor}
+PyObject* q8_workspaces;  // the same of glide_q8_tree_attn
 
 // An exact torch.Tensor or nullptr.
 const at::Tensor* tensor(PyObject* o) { return THPVariable_CheckExact(o) ? &THPVariable_Unpack(o) : nullptr; }
@@ -103,12 +104,12 @@ bool stream_of(const at::Tensor& t, hipStream_t* s, PyObject** handle) {
   return true;
 }
 
-// The kept attention workspace of the device and stream, if it is large
-// enough; `held` keeps it alive until the call has been enqueued (another
+// The kept attention workspace (of `kept`) of the device and stream, if it is
+// large enough; `held` keeps it alive until the call has been enqueued (another
 // thread may replace it meanwhile).  `handle` is consumed.
-bool kept_workspace(const at::Tensor& on, PyObject* handle, size_t need, at::Tensor* held) {
+bool kept_workspace(PyObject* kept, const at::Tensor& on, PyObject* handle, size_t need, at::Tensor* held) {
   PyObject* key = Py_BuildValue("(lN)", (long)on.get_device(), handle);
-  PyObject* ws = key ? PyDict_GetItemWithError(workspaces, key) : nullptr;
+  PyObject* ws = key ? PyDict_GetItemWithError(kept, key) : nullptr;
   Py_XDECREF(key);
   PyErr_Clear();
   const at::Tensor* t = ws ? tensor(ws) : nullptr;
@@ -167,7 +168,7 @@ PyObject* tree_attn(PyObject* const* a, Py_ssize_t n) {
     const size_t need = calls.tree_attn_workspace(B, N, H, GLIDE_HEAD_DIM, cap, splits);
     if (need == 0)
       Py_DECREF(handle);
-    else if (!kept_workspace(*q, handle, need, &ws))
+    else if (!kept_workspace(workspaces, *q, handle, need, &ws))
       return nullptr;
   } else {
     const at::Tensor* w = tensor(a[8]);
@@ -510,7 +511,7 @@ PyObject* q8_tree_attn(PyObject* const* a, Py_ssize_t n) {
     if (need == 0 || q8.capture_id(s)) {
       Py_DECREF(handle);
       if (need) return nullptr;
-    } else if (!kept_workspace(*q, handle, need, &ws)) {
+    } else if (!kept_workspace(q8_workspaces, *q, handle, need, &ws)) {
       return nullptr;
     }
   } else {
@@ -599,11 +600,11 @@ PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t n) {
   Py_RETURN_NONE;
 }
 
-// bind_q8(addresses of the entry points in Q8Calls' order)
+// bind_q8(addresses of the entry points in Q8Calls' order, workspaces)
 PyObject* bind_q8(PyObject*, PyObject* const* args, Py_ssize_t n) {
   constexpr int kCalls = sizeof(Q8Calls) / sizeof(void*);
-  if (n != 1 || !PyTuple_Check(args[0]) || PyTuple_GET_SIZE(args[0]) != kCalls) {
-    PyErr_SetString(PyExc_TypeError, "bind_q8(addresses)");
+  if (n != 2 || !PyTuple_Check(args[0]) || PyTuple_GET_SIZE(args[0]) != kCalls || !PyDict_Check(args[1])) {
+    PyErr_SetString(PyExc_TypeError, "bind_q8(addresses, workspaces)");
     return nullptr;
   }
   void* p[kCalls];
@@ -612,6 +613,9 @@ PyObject* bind_q8(PyObject*, PyObject* const* args, Py_ssize_t n) {
     if (PyErr_Occurred()) return nullptr;
   }
   memcpy(&q8, p, sizeof(q8));
+  Py_INCREF(args[1]);
+  Py_XDECREF(q8_workspaces);
+  q8_workspaces = args[1];
   Py_RETURN_NONE;
 }
 

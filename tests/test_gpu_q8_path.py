@@ -191,6 +191,38 @@ def test_two_graphs_and_eager_calls_at_once():
         assert _same(_results(s), w)
 
 
+def test_workspaces_of_the_two_attentions_are_apart():
+    """A captured glide_tree_attn goes on using the workspace that its stream's
+    eager calls left: neither a larger glide_q8_tree_attn nor what is allocated
+    after it takes that memory's place, and every replay stays the same."""
+    require_gpu()
+    dev = torch.device("cuda")
+    side = torch.cuda.Stream()
+    B, N, H, L = 1, 5, 4, 2000
+    q = cpu_normal((B, N, H, 128), 90, BF).cuda()
+    k, v = cpu_normal((B, H, L + N, 128), 91, BF).cuda(), cpu_normal((B, H, L + N, 128), 92, BF).cuda()
+    lens, out = ints([L]), torch.empty_like(q)
+    cache, many = junk_cache(1, 32, 4096, "e4m3"), cpu_normal((1, 64, 32, 128), 93, BF).cuda()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        glide.glide_tree_attn(q, k, v, lens, None, out)
+        want = out.clone()
+        kept = glide.attn_workspace(B, N, H, L + N, 0, dev)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            glide.glide_tree_attn(q, k, v, lens, None, out)
+        glide.glide_q8_tree_attn(many, cache, ints([0]), None, torch.empty_like(many))
+        own = glide.q8_attn_workspace(1, 64, 32, 32, 4096, 0, dev)
+        assert own.numel() > kept.numel() and glide.attn_workspace(B, N, H, L + N, 0, dev) is kept
+        junk = [torch.full((kept.numel(),), 0xFF, dtype=torch.uint8, device=dev) for _ in range(4)]
+        for i in range(3):
+            out.fill_(float("nan"))
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(out, want), i
+    assert len(junk) == 4
+
+
 def test_an_explicit_stream():
     require_gpu()
     s = _step_state(130, L=2500)
