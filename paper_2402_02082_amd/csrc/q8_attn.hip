@@ -421,7 +421,9 @@ __device__ __forceinline__ void join_states(const Q8AttnArgs& a, int first, int 
   const int quads = (rows + 3) / 4;
   const int parts = quads == 1 ? WAVES : (quads == 2 ? WAVES / 2 : (quads <= 4 ? WAVES / 4 : 1));  // waves that share a row
   const int part = wave % parts, d = lane % 16 * 8;
-  for (int quad = wave / parts; quad < quads; quad += WAVES / parts) {
+  // waves that share rows meet at a barrier, so all of them take one turn, with
+  // rows past the last (zeros, by the descriptors) or without
+  for (int quad = wave / parts; quad < (parts > 1 ? WAVES / parts : quads); quad += WAVES / parts) {
     const int row = 4 * quad + lane / 16;
     const bool live = row < rows;
     float M = neg_inf(), L = 0.f, o[8];
@@ -454,7 +456,7 @@ __device__ __forceinline__ void join_states(const Q8AttnArgs& a, int first, int 
         M = m;
       }
     }
-    if (parts > 1) {  // up to 16 rows, and one turn of this loop
+    if (parts > 1) {  // up to 16 rows
       const int slot = row;
       lds.m[part][slot] = M, lds.l[part][slot] = L;
 #pragma unroll

@@ -169,6 +169,20 @@ def test_plans(B, H, Hk, N, top):
         assert torch.equal(run(q, cache, lens, par), out)
 
 
+@pytest.mark.parametrize("pairs", [4, 140])
+@pytest.mark.parametrize("N", [3, 7, 10, 13])
+def test_rows_that_do_not_fill_the_waves(pairs, N):
+    """The runs' states joined by four and by eight waves that share rows, of which
+    some have a turn without rows (9 to 12 rows for eight waves)."""
+    require_gpu()
+    say("joined rows", pairs, N)
+    lens = [330, 100]
+    cache, k, v = fill(2, pairs // 2, lens, "e4m3", 54)
+    q = cpu_normal((2, N, pairs // 2, 128), 55, BF).cuda()
+    for splits in (3, 20):
+        check(run(q, cache, lens, None, max_splits=splits), q, k, v, lens, "e4m3", pairs={(0, 0), (1, pairs // 2 - 1)})
+
+
 @pytest.mark.parametrize("kind", KINDS)
 def test_peaked_scores(kind):
     """Queries times 24: the reference maximum is passed by far and often."""
