@@ -87,24 +87,23 @@ __device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d) {
   return (uint32_t)w;
 }
 
-// Quantises and writes K or V of a block, called by a whole wave; row(t) is where
-// token t's values start.  Lane 16 g + c takes of K, for each (kt, h), token
+// Quantises and writes K or V of a block, called by a whole wave; at(t, d) is where
+// token t's values from dim d on are.  Lane 16 g + c takes of K, for each (kt, h), token
 // 16 kt + c, dims 64 h + 16 g + (0..15): x[4 kt + 2 h + half]; of V the tokens
 // 16 (i / 4) + 4 g + i % 4, dims 8 c + (0..7): x[i].
-template <bool INT8, class Row>
-__device__ __forceinline__ void quantise_part(bool v, int lane, uint8_t* part, float* scale_out, Row row) {
+template <bool INT8, class At>
+__device__ __forceinline__ void quantise_part(bool v, int lane, uint8_t* part, float* scale_out, At at) {
   const int c = lane & 15, g = lane >> 4;
   u32x4_t x[8];
   if (v) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = *(const u32x4_t*)(row(16 * (i >> 2) + 4 * g + (i & 3)) + 8 * c);
+    for (int i = 0; i < 8; ++i) x[i] = *(const u32x4_t*)at(16 * (i >> 2) + 4 * g + (i & 3), 8 * c);
   } else {
 #pragma unroll
-    for (int kt = 0; kt < 2; ++kt) {
-      const uint16_t* p = row(16 * kt + c) + 16 * g;
+    for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) x[4 * kt + i] = *(const u32x4_t*)(p + 64 * (i >> 1) + 8 * (i & 1));
-    }
+      for (int i = 0; i < 4; ++i)
+        x[4 * kt + i] = *(const u32x4_t*)at(16 * kt + c, 16 * g + 64 * (i >> 1) + 8 * (i & 1));
   }
   uint32_t top = 0;
 #pragma unroll
@@ -175,9 +174,9 @@ __global__ __launch_bounds__(kThreads) void q8_append_kernel(Q8AppendArgs a) {
   if ((block + 1) * kQ8Block <= end) {
     const size_t at = head * a.n_blocks + block;
     quantise_part<INT8>(m, lane, a.cache.blocks + at * kQ8BlockBytes + m * kQ8PartBytes, a.cache.scales + at * 2 + m,
-                        [&](int t) {
+                        [&](int t, int d) {
                           const int tok = block * kQ8Block + t;
-                          return tok < L ? held + (tok & (kQ8Tail - 1)) * kHeadDim : from + (tok - L) * a.st;
+                          return (tok < L ? held + (tok & (kQ8Tail - 1)) * kHeadDim : from + (tok - L) * a.st) + d;
                         });
   }
   if (i > 0) return;
@@ -269,19 +268,17 @@ __global__ __launch_bounds__(kThreads) void q8_read_kernel(Q8ReadArgs a) {
 // those rows; what is left behind them (at most 31 rows) moves to its place in
 // the ring, all of it read before any of it is written.
 template <bool INT8>
-__global__ __launch_bounds__(kThreads) void q8_commit_kernel(Q8CommitArgs a) {
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(8))) void q8_commit_kernel(Q8CommitArgs a) {
   const int b = blockIdx.y, lane = threadIdx.x & 63;
   const int id = kWaves * blockIdx.x + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = id >> 1, m = id & 1;
   const Q8Cache& cache = a.cache[blockIdx.z];
+  const int on_path = a.path ? a.path[(size_t)b * a.N + min(lane, a.N - 1)] : lane;
+  const int len = a.seq_lens[b], accepted = a.accept_len[b];
   // node at each depth; nodes outside [0, N) count as the chain's
-  int node = lane;
-  if (a.path && lane < a.N) {
-    const int p = a.path[(size_t)b * a.N + lane];
-    if (p >= 0 && p < a.N) node = p;
-  }
+  const int node = lane < a.N && on_path >= 0 && on_path < a.N ? on_path : lane;
   const int cap = a.n_blocks * kQ8Block;
-  const int L = min(max(a.seq_lens[b], 0), cap);
-  const int n = min(min(max(a.accept_len[b], 0), a.N), cap - L);
+  const int L = __builtin_amdgcn_readfirstlane(min(max(len, 0), cap));
+  const int n = __builtin_amdgcn_readfirstlane(min(min(max(accepted, 0), a.N), cap - L));
   const int end = L + n;
   if (id == 0 && blockIdx.z == 0 && lane == 0) a.seq_lens_out[b] = end;
   if (n == 0 || h >= a.H) return;
@@ -296,26 +293,25 @@ __global__ __launch_bounds__(kThreads) void q8_commit_kernel(Q8CommitArgs a) {
   for (int block = L / kQ8Block; block < whole; ++block) {
     const size_t at = head * a.n_blocks + block;
     quantise_part<INT8>(m, lane, cache.blocks + at * kQ8BlockBytes + m * kQ8PartBytes, cache.scales + at * 2 + m,
-                        [&](int t) { return rows + held(block * kQ8Block + t) * kHeadDim; });
+                        [&](int t, int d) { return rows + (unsigned)(held(block * kQ8Block + t) * kHeadDim + d); });
   }
   // The rows left, four a load; a path that starts down the chain keeps the rows
   // that are in place.
   const int first = max(L, whole * kQ8Block), left = end - first;
   const int dim = lane % kChunks * 8, q = lane / kChunks;
   u32x4_t x[kQ8Block / 4];
-  int to[kQ8Block / 4], source[kQ8Block / 4];
+  bool moves[kQ8Block / 4];
 #pragma unroll
   for (int j = 0; j < kQ8Block / 4; ++j) {
     if (4 * j >= left) break;
-    const int tok = first + 4 * j + q;
-    source[j] = held(tok);
-    to[j] = 4 * j + q < left ? tok & (kQ8Tail - 1) : source[j];
-    if (to[j] != source[j]) x[j] = *(const u32x4_t*)(rows + source[j] * kHeadDim + dim);
+    const int tok = first + 4 * j + q, source = held(tok);
+    moves[j] = 4 * j + q < left && source != (tok & (kQ8Tail - 1));
+    if (moves[j]) x[j] = *(const u32x4_t*)(rows + (unsigned)(source * kHeadDim + dim));
   }
 #pragma unroll
   for (int j = 0; j < kQ8Block / 4; ++j) {
     if (4 * j >= left) break;
-    if (to[j] != source[j]) *(u32x4_t*)(rows + to[j] * kHeadDim + dim) = x[j];
+    if (moves[j]) *(u32x4_t*)(rows + (unsigned)(((first + 4 * j + q) & (kQ8Tail - 1)) * kHeadDim + dim)) = x[j];
   }
 }
 
