@@ -33,6 +33,17 @@
 //    bfloat16 the rounding of P alone is as far off as that of the output.
 // Ring rows are bfloat16: their products take bfloat16 operands, P as the sum
 // of two.  Sums, maxima and outputs are float32.
+//
+// Bound: the memory where keys are long (sixteen sequences of 16 to 32 thousand
+// tokens, 32 heads, five rows: 3.23 GB in 465 us, 6.9 TB/s; the matrix cores busy
+// a tenth of it).  Short ones pay about 10 us around the stream: 2.5 for the launch
+// and finding the run, 2 for the queries and the first blocks, 2 to 4 for ring
+// rows, 1 to 3 for the joins (four sequences of 40 heads, 32 tree rows, 110 MB:
+// 27 us; sixteen sequences, four query heads to each of eight cached ones, 168 MB:
+// 35).  A 7B layer's chain of five behind 512 tokens takes 7.5 us.  64 rows are
+// bound by the conversions, the softmax and the matrix instructions in turn
+// (eight sequences of 52 heads, 64 tree rows: 165 us, 4.1 TB/s, vector
+// instructions 45 % and matrix instructions 23 % of the cycles).
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -250,17 +261,13 @@ __device__ __forceinline__ void load_v(RawUnit& f, __amdgpu_buffer_rsrc_t r, int
         u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(r, lane * 16 + kQ8PartBytes + 1024 * i, 0, CPOL));
 }
 
-// Tokens and units of sequence b.  A sequence without keys counts as one unit,
-// so that some workgroup writes its zeros.
-struct Seq {
-  int L, end, units;
-};
-__device__ __forceinline__ Seq sequence(const Q8AttnArgs& a, bool tree, int b) {
-  Seq s;
-  s.L = min(max(a.seq_lens[b], 0), a.n_blocks * kQ8Block);
-  s.end = s.L + (tree ? a.N : 0);
-  s.units = max(1, (s.end + kQ8Block - 1) / kQ8Block);
-  return s;
+// Tokens of sequence b, and units of a sequence of L tokens.  One without keys
+// counts as one unit, so that some workgroup writes its zeros.
+__device__ __forceinline__ int tokens(const Q8AttnArgs& a, int b) {
+  return min(max(a.seq_lens[b], 0), a.n_blocks * kQ8Block);
+}
+__device__ __forceinline__ int units_of(const Q8AttnArgs& a, bool tree, int L) {
+  return max(1, (L + (tree ? a.N : 0) + kQ8Block - 1) / kQ8Block);
 }
 
 // Inclusive sum over a wave, by moves inside and across its 16-lane rows.
@@ -277,10 +284,10 @@ __device__ __forceinline__ int scan64(int v) {
   return add_moved<0x143, 0xC>(v);  // lane 31 to the upper half
 }
 
-// The run of a workgroup: units [u0, u1) of (b, hk), the first of `n` runs of
-// that pair being number `first` and the others a.H_kv apart.
+// The run of a workgroup: units [u0, u1) of (b, hk) with L tokens, the first of
+// `n` runs of that pair being number `first` and the others a.H_kv apart.
 struct Run {
-  int b, hk, u0, u1, n, first;
+  int b, hk, L, u0, u1, n, first;
 };
 
 // Runs of a pair of so many units, of up to `per` units each.
@@ -290,7 +297,7 @@ __device__ __forceinline__ int runs_of(const Q8AttnArgs& a, int units, int per) 
 
 // Units of sequence b, 0 past the last; `mine`: of the lane's among the first 64.
 __device__ __forceinline__ int units_at(const Q8AttnArgs& a, bool tree, int b, int lane, int mine) {
-  return b == lane ? mine : (b < a.B ? sequence(a, tree, b).units : 0);
+  return b == lane ? mine : (b < a.B ? units_of(a, tree, tokens(a, b)) : 0);
 }
 
 // Sum over all sequences of their units (per == 0) or runs.  Called by whole
@@ -304,9 +311,13 @@ __device__ __forceinline__ int sum_of(const Q8AttnArgs& a, bool tree, int per, i
   return __builtin_amdgcn_readlane(scan64(sum), 63);
 }
 
-// Run number `run`; false past the last.  Called by whole waves.
+// Run number `run`; false past the last.  Called by whole waves.  Each lane has
+// the length of one of the first 64 sequences, so that most calls read the lengths
+// once.
 __device__ __forceinline__ bool find_run(const Q8AttnArgs& a, bool tree, int run, int lane, Run* r) {
   int b = 0, before = 0, per = 1;
+  int len = 0;
+  if (a.B > 1) len = tokens(a, min(lane, a.B - 1));
   if (a.splits) {
     b = run / (a.splits * a.H_kv);
     if (b >= a.B) return false;
@@ -314,7 +325,6 @@ __device__ __forceinline__ bool find_run(const Q8AttnArgs& a, bool tree, int run
     if (a.splits == 1 && a.B >= 2 && a.B <= 64) {
       // the b-th longest sequence (of equals the first): the longest start first,
       // and the shorter ones fill in as CUs come free
-      const int len = lane < a.B ? a.seq_lens[lane] : 0;
       int rank = 0;
       for (int j = 0; j < a.B; ++j) {
         const int lj = __builtin_amdgcn_readlane(len, j);
@@ -323,13 +333,13 @@ __device__ __forceinline__ bool find_run(const Q8AttnArgs& a, bool tree, int run
       b = __ffsll((long long)__ballot(lane < a.B && rank == b)) - 1;
     }
   } else if (a.B == 1) {
-    const int units = sequence(a, tree, 0).units;
+    const int units = units_of(a, tree, __builtin_amdgcn_readfirstlane(tokens(a, 0)));
     const int most = units * a.H_kv >= a.target * a.long_run ? a.target : (a.target + 1) / 2, n = max(1, most / a.H_kv);
     per = max((units + n - 1) / n, a.min_units);
   } else {
     // about the fewest units a run with which no more than `most` runs come out;
     // n pairs of any lengths have about n / 2 runs more than whole ones would be
-    const int mine = lane < a.B ? sequence(a, tree, lane).units : 0;
+    const int mine = lane < a.B ? units_of(a, tree, len) : 0;
     const int total = sum_of(a, tree, 0, lane, mine) * a.H_kv;
     const int most = total >= a.target * a.long_run ? a.target : (a.target + 1) / 2;
     const int whole = max(1, most - a.B * a.H_kv / 2);
@@ -351,11 +361,12 @@ __device__ __forceinline__ bool find_run(const Q8AttnArgs& a, bool tree, int run
     if (!found) return false;
   }
   b = __builtin_amdgcn_readfirstlane(b);
-  const int units = __builtin_amdgcn_readfirstlane(sequence(a, tree, b).units);
+  const int L = __builtin_amdgcn_readfirstlane(a.B > 1 && a.B <= 64 ? __builtin_amdgcn_readlane(len, b) : tokens(a, b));
+  const int units = units_of(a, tree, L);
   const int n = runs_of(a, units, per), rest = run - before, i = rest / a.H_kv;
   if (i >= n) return false;  // (a single sequence: past its last run)
   const int size = (units + n - 1) / n;
-  r->b = b, r->hk = rest - i * a.H_kv, r->n = n, r->first = before + r->hk;
+  r->b = b, r->hk = rest - i * a.H_kv, r->L = L, r->n = n, r->first = before + r->hk;
   r->u0 = min(units, i * size), r->u1 = min(units, r->u0 + size);
   return true;
 }
@@ -434,10 +445,10 @@ __device__ __forceinline__ void join_states(const Q8AttnArgs& a, int first, int 
       f32x4_t x[kBatch][2];
 #pragma unroll
       for (int j = 0; j < kBatch; ++j) {
-        const int i = min(s0 + j * parts, n - 1);
+        const int i = s0 + j * parts, live_rows = i < n ? rows : 0;  // none: no memory is read
         const size_t at = ((size_t)(first + i * a.H_kv) * a.groups + grp) * kRows;
-        const __amdgpu_buffer_rsrc_t rm = state_rsrc(a.part_ml + at, rows * 8);
-        const __amdgpu_buffer_rsrc_t ro = state_rsrc(a.part_o + at * kD, rows * kD * 4);
+        const __amdgpu_buffer_rsrc_t rm = state_rsrc(a.part_ml + at, live_rows * 8);
+        const __amdgpu_buffer_rsrc_t ro = state_rsrc(a.part_o + at * kD, live_rows * kD * 4);
         ml[j] = __builtin_bit_cast(f32x2_t, __builtin_amdgcn_raw_buffer_load_b64(rm, row * 8, 0, kDeviceScope));
 #pragma unroll
         for (int h = 0; h < 2; ++h)
@@ -446,7 +457,7 @@ __device__ __forceinline__ void join_states(const Q8AttnArgs& a, int first, int 
       }
 #pragma unroll
       for (int j = 0; j < kBatch; ++j) {
-        if (s0 + j * parts >= n || ml[j][1] == 0.f) continue;  // a run that saw no key
+        if (ml[j][1] == 0.f) continue;  // a run that saw no key, or none
         const float m = fmaxf(M, ml[j][0]);
         const float ref = m == neg_inf() ? 0.f : m;
         const float keep = fast_exp2(M - ref), w = fast_exp2(ml[j][0] - ref) * ml[j][1];
@@ -507,17 +518,21 @@ void q8_attn_kernel(Q8AttnArgs a) {
   // Query rows: row r is node r / G of query head hk * G + r % G.  MFMA step
   // 2 h + e holds dims 64 h + 16 g + 8 e + (0..7).  A single sequence's are
   // requested before its length is known.
-  int node[NT];
+  int node[NT], q_row[NT];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    const int r = row0 + 16 * nt + c;
+    node[nt] = r < R ? r / G : 0;
+    q_row[nt] = r < R ? node[nt] * a.H + (r - node[nt] * G) : -1;
+  }
   u32x4_t qf[NT][4];
   auto load_queries = [&](int b, int hk) {
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-      const int r = row0 + 16 * nt + c;
-      node[nt] = r < R ? r / G : 0;
-      const uint16_t* q = a.q + (((size_t)b * a.N + node[nt]) * a.H + hk * G + (r - node[nt] * G)) * kD;
+      const uint16_t* q = a.q + ((size_t)b * a.N * a.H + q_row[nt] + hk * G) * kD;
 #pragma unroll
       for (int st = 0; st < 4; ++st)
-        qf[nt][st] = r < R ? *(const u32x4_t*)(q + 64 * (st >> 1) + 16 * g + 8 * (st & 1)) : u32x4_t{0, 0, 0, 0};
+        qf[nt][st] = q_row[nt] >= 0 ? *(const u32x4_t*)(q + 64 * (st >> 1) + 16 * g + 8 * (st & 1)) : u32x4_t{0, 0, 0, 0};
     }
   };
   if (a.B == 1) load_queries(0, run % a.H_kv);
@@ -525,8 +540,7 @@ void q8_attn_kernel(Q8AttnArgs a) {
   Run rn;
   if (!find_run(a, TREE, run, lane, &rn)) return;
   const int b = rn.b, hk = rn.hk, u0 = rn.u0, u1 = rn.u1;
-  const Seq seq = sequence(a, TREE, b);
-  const int L = __builtin_amdgcn_readfirstlane(seq.L), end = __builtin_amdgcn_readfirstlane(seq.end);
+  const int L = rn.L, end = L + (TREE ? a.N : 0);
   const int whole = L / kQ8Block;
   const size_t head = (size_t)b * a.H_kv + hk;
   const uint8_t* blocks = a.cache.blocks + head * a.n_blocks * (size_t)kQ8BlockBytes;
@@ -559,10 +573,28 @@ void q8_attn_kernel(Q8AttnArgs a) {
   };
   if (a.B > 1) load_queries(b, hk);
 
-  // The first blocks are requested now, unless the wave has ring rows and no
-  // registers to hold the blocks through their scores.
-  const bool later = kStages == 1 && ring;
-  if (!later) prefetch();
+  const int j0 = (max(u0, whole) + kKeyWaves - 1 - kw) * kQ8Block;  // the ring unit's first token
+  int parent = -1;
+  u32x4_t kf[2][4], v[8];
+  auto load_ring = [&] {
+    if (TREE) parent = a.parents[(size_t)b * a.N + min(lane, a.N - 1)];
+    const uint16_t* kt_rows = a.cache.tail + head * kQ8TailElems + (j0 & (kQ8Tail - 1)) * kD;
+    const uint16_t* vt_rows = kt_rows + kQ8Tail * kD;
+#pragma unroll
+    for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+      for (int st = 0; st < 4; ++st)
+        kf[kt][st] = *(const u32x4_t*)(kt_rows + (16 * kt + c) * kD + 64 * (st >> 1) + 16 * g + 8 * (st & 1));
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = *(const u32x4_t*)(vt_rows + (16 * (i >> 2) + 4 * g + (i & 3)) * kD + 8 * c);
+  };
+
+  // Ring rows are requested first, since what is waited for comes back in order,
+  // and the first blocks behind them; a wave with registers for one stage only
+  // requests the blocks behind the ring rows' scores.
+  constexpr bool kTogether = kStages > 1;
+  if (kTogether && ring) load_ring();
+  if (kTogether || !ring) prefetch();
 
   RowState sm[NT];
   f32x4_t acc[NT][8];
@@ -575,23 +607,11 @@ void q8_attn_kernel(Q8AttnArgs a) {
 
   // Ring rows, taken first.
   if (ring) {
-    const int j0 = (max(u0, whole) + kKeyWaves - 1 - kw) * kQ8Block;
-    int parent = -1;
-    if (TREE && lane < a.N) parent = a.parents[(size_t)b * a.N + lane];
-    const uint16_t* kt_rows = a.cache.tail + head * kQ8TailElems + (j0 & (kQ8Tail - 1)) * kD;
-    const uint16_t* vt_rows = kt_rows + kQ8Tail * kD;
-    u32x4_t kf[2][4], v[8];
-#pragma unroll
-    for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-      for (int st = 0; st < 4; ++st)
-        kf[kt][st] = *(const u32x4_t*)(kt_rows + (16 * kt + c) * kD + 64 * (st >> 1) + 16 * g + 8 * (st & 1));
+    if (!kTogether) load_ring();
     uint32_t top = 0;  // the largest size of the unit's values
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const int row = 16 * (i >> 2) + 4 * g + (i & 3);
-      v[i] = *(const u32x4_t*)(vt_rows + row * kD + 8 * c);
-      if (j0 + row >= end) v[i] = u32x4_t{0, 0, 0, 0};  // rows that hold no token
+      if (j0 + 16 * (i >> 2) + 4 * g + (i & 3) >= end) v[i] = u32x4_t{0, 0, 0, 0};  // rows that hold no token
 #pragma unroll
       for (int e = 0; e < 4; ++e) top = max_size(top, v[i][e]);
     }
@@ -610,7 +630,7 @@ void q8_attn_kernel(Q8AttnArgs a) {
     top = wave_max(top);
     const float ls = __builtin_amdgcn_logf(__uint_as_float(top << 16)) - 8.f;  // as if the largest were a code of 256
     uint64_t mine = 0;  // ancestor mask of node `lane`
-    if (TREE) mine = ancestor_mask(parent, lane);
+    if (TREE) mine = ancestor_mask(lane < a.N ? parent : -1, lane);
     u32x4_t vt[8];  // V^T operands: tile t holds dim 8 c + t of the lane's eight tokens
 #pragma unroll
     for (int w = 0; w < 4; ++w)
@@ -630,7 +650,7 @@ void q8_attn_kernel(Q8AttnArgs a) {
           x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(kf[kt][st]), as_bf16x8(qf[nt][st]), x, 0, 0, 0);
         s[kt][nt] = x;
       }
-    if (later) prefetch();
+    if (!kTogether) prefetch();
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       uint64_t anc = 0;
