@@ -656,6 +656,7 @@ int glide_q8_tree_attn(const void* q, const glide_q8_cache* cache, const int32_t
   a.N = N;
   a.H = H;
   a.H_kv = H_kv;
+  a.G = H / H_kv;
   a.n_blocks = L_cap / glide::kQ8Block;
   a.groups = p.groups;
   a.splits = p.splits;

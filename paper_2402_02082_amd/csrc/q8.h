@@ -98,7 +98,8 @@ struct Q8AttnArgs {
   unsigned* counters;  // arrival counters of pairs that lie in several runs
   float* part_o;    // [runs, groups, rows, D]: normalised outputs
   float2* part_ml;  // [runs, groups, rows]: (max in log2 units, sum)
-  int B, N, H, H_kv, n_blocks, groups, splits, target, min_units, whole_units, long_run, runs;
+  int B, N, H, H_kv, G, n_blocks, groups, splits,  // G: query heads a cached one
+      target, min_units, whole_units, long_run, runs;
   float scale_log2;
 };
 hipError_t launch_q8_attn(const Q8AttnArgs& a, bool int8, int rows, int waves, hipStream_t stream);

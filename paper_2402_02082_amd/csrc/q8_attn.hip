@@ -203,12 +203,11 @@ __device__ __forceinline__ void softmax_unit(float (&x)[8], RowState& st, f32x4_
   st.l += ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
 }
 
-// Infinities and NaN of a unit's values reach only the rows that see them:
-// takes them out of the eight tokens w of a V^T operand (0 times infinity would
-// be NaN) and returns what rows that see one get added, an infinity of its sign
-// (of both signs for NaN, which gives NaN).  seen: bit per token of the lane.
-__device__ __forceinline__ f32x4_t add_not_finite(u32x4_t& w, uint32_t seen) {
-  u32x4_t pos, neg, vis;
+// Infinities and NaN of a unit's values reach only the rows that see them.  They
+// are taken out of the eight tokens w of a V^T operand (0 times infinity would be
+// NaN), and rows that see one get an infinity of its sign added (of both signs for
+// NaN, which gives NaN): ones in pos and neg mark them.
+__device__ __forceinline__ void take_not_finite(u32x4_t& w, u32x4_t& pos, u32x4_t& neg) {
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     pos[e] = neg[e] = 0;
@@ -222,8 +221,14 @@ __device__ __forceinline__ f32x4_t add_not_finite(u32x4_t& w, uint32_t seen) {
         w[e] &= ~(0xffffu << hi);
       }
     }
-    vis[e] = ((seen >> (2 * e)) & 1 ? 0x3f80u : 0u) | ((seen >> (2 * e + 1)) & 1 ? 0x3f800000u : 0u);
   }
+}
+// What a query column gets added; seen: bit per token of the lane.
+__device__ __forceinline__ f32x4_t add_not_finite(u32x4_t pos, u32x4_t neg, uint32_t seen) {
+  u32x4_t vis;
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    vis[e] = ((seen >> (2 * e)) & 1 ? 0x3f80u : 0u) | ((seen >> (2 * e + 1)) & 1 ? 0x3f800000u : 0u);
   const f32x4_t zero = {0.f, 0.f, 0.f, 0.f};
   const f32x4_t up = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(pos), as_bf16x8(vis), zero, 0, 0, 0);
   const f32x4_t dn = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(neg), as_bf16x8(vis), zero, 0, 0, 0);
@@ -512,7 +517,7 @@ void q8_attn_kernel(Q8AttnArgs a) {
   // apart, on the same XCD and so on the same L2, which they share its keys in.
   const int grp = a.groups == 1 ? 0 : blockIdx.x / 8 % a.groups;
   const int run = a.groups == 1 ? blockIdx.x : blockIdx.x / (8 * a.groups) * 8 + blockIdx.x % 8;
-  const int G = a.H / a.H_kv, R = a.N * G, row0 = grp * kRows + rg * 16 * NT;
+  const int G = a.G, R = a.N * G, row0 = grp * kRows + rg * 16 * NT;
   __shared__ JoinLds<WAVES, 16 * NT> lds;
 
   // Query rows: row r is node r / G of query head hk * G + r % G.  MFMA step
@@ -521,9 +526,9 @@ void q8_attn_kernel(Q8AttnArgs a) {
   int node[NT], q_row[NT];
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
-    const int r = row0 + 16 * nt + c;
-    node[nt] = r < R ? r / G : 0;
-    q_row[nt] = r < R ? node[nt] * a.H + (r - node[nt] * G) : -1;
+    const unsigned r = row0 + 16 * nt + c < R ? row0 + 16 * nt + c : 0;  // rows past the last: copies of the first
+    node[nt] = r / (unsigned)G;
+    q_row[nt] = node[nt] * (a.H - G) + r;
   }
   u32x4_t qf[NT][4];
   auto load_queries = [&](int b, int hk) {
@@ -531,8 +536,7 @@ void q8_attn_kernel(Q8AttnArgs a) {
     for (int nt = 0; nt < NT; ++nt) {
       const uint16_t* q = a.q + ((size_t)b * a.N * a.H + q_row[nt] + hk * G) * kD;
 #pragma unroll
-      for (int st = 0; st < 4; ++st)
-        qf[nt][st] = q_row[nt] >= 0 ? *(const u32x4_t*)(q + 64 * (st >> 1) + 16 * g + 8 * (st & 1)) : u32x4_t{0, 0, 0, 0};
+      for (int st = 0; st < 4; ++st) qf[nt][st] = *(const u32x4_t*)(q + 64 * (st >> 1) + 16 * g + 8 * (st & 1));
     }
   };
   if (a.B == 1) load_queries(0, run % a.H_kv);
@@ -611,7 +615,7 @@ void q8_attn_kernel(Q8AttnArgs a) {
     uint32_t top = 0;  // the largest size of the unit's values
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      if (j0 + 16 * (i >> 2) + 4 * g + (i & 3) >= end) v[i] = u32x4_t{0, 0, 0, 0};  // rows that hold no token
+      v[i] &= j0 + 16 * (i >> 2) + 4 * g + (i & 3) < end ? ~0u : 0u;  // rows that hold no token: zeros
 #pragma unroll
       for (int e = 0; e < 4; ++e) top = max_size(top, v[i][e]);
     }
@@ -651,38 +655,47 @@ void q8_attn_kernel(Q8AttnArgs a) {
         s[kt][nt] = x;
       }
     if (!kTogether) prefetch();
+    u32x4_t ph[NT], pl[NT];
+    uint32_t seen[NT];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       uint64_t anc = 0;
       if (TREE)
         anc = ((uint64_t)(uint32_t)__shfl((uint32_t)(mine >> 32), node[nt]) << 32) | (uint32_t)__shfl((uint32_t)mine, node[nt]);
       float x[8];
-      uint32_t seen = 0;
+      seen[nt] = 0;
 #pragma unroll
-      for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int j = j0 + 16 * kt + 4 * g + r;
-          const bool vis = j < L || (TREE && j < end && ((anc >> (j - L)) & 1));
-          seen |= (vis ? 1u : 0u) << (4 * kt + r);
-          x[4 * kt + r] = vis ? s[kt][nt][r] : neg_inf();
-        }
+      for (int i = 0; i < 8; ++i) {
+        const int j = j0 + 16 * (i >> 2) + 4 * g + (i & 3);
+        uint32_t vis = j < L;
+        if (TREE) vis |= (uint32_t)(anc >> ((j - L) & 63)) & (uint32_t)(j >= L) & (uint32_t)(j < end);
+        seen[nt] |= vis << i;
+        x[i] = vis ? s[i >> 2][nt][i & 3] : neg_inf();
+      }
       softmax_unit(x, sm[nt], acc[nt], a.scale_log2, ls);
-      u32x4_t ph, pl;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const float p0 = x[2 * e] * sm[nt].c, p1 = x[2 * e + 1] * sm[nt].c;
-        ph[e] = pack_bf16x2(p0, p1);
-        pl[e] = pack_bf16x2(p0 - __uint_as_float(ph[e] << 16), p1 - __uint_as_float(ph[e] & 0xffff0000u));
-      }
-#pragma unroll
-      for (int t = 0; t < 8; ++t) {
-        u32x4_t w = vt[t];
-        if (odd) acc[nt][t] += add_not_finite(w, seen);
-        acc[nt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(w), as_bf16x8(ph), acc[nt][t], 0, 0, 0);
-        acc[nt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(w), as_bf16x8(pl), acc[nt][t], 0, 0, 0);
+        ph[nt][e] = pack_bf16x2(p0, p1);
+        pl[nt][e] = pack_bf16x2(p0 - __uint_as_float(ph[nt][e] << 16), p1 - __uint_as_float(ph[nt][e] & 0xffff0000u));
       }
     }
+    if (odd) {
+#pragma unroll
+      for (int t = 0; t < 8; ++t) {
+        u32x4_t pos, neg;
+        take_not_finite(vt[t], pos, neg);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) acc[nt][t] += add_not_finite(pos, neg, seen[nt]);
+      }
+    }
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int t = 0; t < 8; ++t) {
+        acc[nt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(vt[t]), as_bf16x8(ph[nt]), acc[nt][t], 0, 0, 0);
+        acc[nt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(vt[t]), as_bf16x8(pl[nt]), acc[nt][t], 0, 0, 0);
+      }
   }
 
   // From here on q is fp16: of q * 2^(14 - e), e the exponent of the row's largest.
