@@ -14,7 +14,7 @@
 // there; of the others each run leaves a state, counts itself in, and the one
 // that completes the pair joins the states in order, whichever that is: one
 // launch.
-// A workgroup's waves (eight, or four where pairs are split) take units in turn,
+// A workgroup's waves (eight, or four for few pairs of few rows) take units in turn,
 // each for all of the group's rows (up to 32 rows; 64 rows: four waves for each
 // half, the second read of a unit then comes from L2), so each code is converted
 // by one or two waves.
@@ -873,22 +873,25 @@ Q8AttnPlan plan_q8_attn(int B, int N, int H, int H_kv, int n_blocks, int max_spl
     p.runs = pairs;
     return p;
   }
+  // Up to 16 rows of few pairs take four waves, two workgroups a CU; all others
+  // eight, one a CU (32 rows of 16 long pairs with four: 62 us, with eight 45).
   const bool few = wgs <= kNumCU / 2;
-  // 64 rows take eight waves, one workgroup a CU; fewer rows of few pairs four waves, two.
-  if (p.rows < 64 && few) p.waves = 4;
+  if (p.rows == 16 && few) p.waves = 4;
   if (max_splits > 0) {
     p.splits = (int)min((long)max_splits, most);
     p.runs = pairs * p.splits;
   } else {
     // Joining runs takes 3 us, so short pairs are not split, and where workgroups
-    // take more than half of the CUs only those that are long for their call are.
-    p.whole_units = few ? 24 : 48;
-    p.min_units = few ? 8 : 16;
-    // Up to one run a CU; of few pairs two from 32 units a run on (7B layer of 2048
+    // take more than half of the CUs only those that are long for their call are
+    // (one sequence of 32 heads, five rows, 25 units: 7.6 us whole, 8.5 split; of 40
+    // heads, 32 rows: 32 units 12.4 and 13.3, 48 units 15.0 and 14.1).
+    p.whole_units = few ? (p.waves == 4 ? 28 : 40) : 48;
+    p.min_units = p.waves == 4 ? 8 : 16;
+    // Up to one run a CU; of four waves two from 32 units a run on (7B layer of 2048
     // tokens: 8 runs a pair 10.4 us, 9 14.4; one head group of 60000 tokens, 32
     // runs a pair 25.7, 63 28.2; 128 pairs of 160 units 36.8 with one, 35.0 with two).
-    p.target = max(1, (few ? 2 : 1) * kNumCU / p.groups);
-    p.long_run = few ? 32 : 0;
+    p.target = max(1, (p.waves == 4 ? 2 : 1) * kNumCU / p.groups);
+    p.long_run = p.waves == 4 ? 32 : 0;
     p.runs = max(pairs, min(pairs + p.target, pairs * ((most + p.min_units - 1) / p.min_units)));
     if (most <= p.whole_units) return p;  // no pair will be split: no states
   }
@@ -901,7 +904,7 @@ Q8AttnPlan plan_q8_attn(int B, int N, int H, int H_kv, int n_blocks, int max_spl
 
 hipError_t launch_q8_attn(const Q8AttnArgs& a, bool int8, int rows, int waves, hipStream_t stream) {
   if (rows == 16) return waves == 4 ? launch_rows<4, 1, 1>(a, int8, stream) : launch_rows<8, 1, 1>(a, int8, stream);
-  if (rows == 32) return waves == 4 ? launch_rows<4, 2, 1>(a, int8, stream) : launch_rows<8, 2, 1>(a, int8, stream);
+  if (rows == 32) return launch_rows<8, 2, 1>(a, int8, stream);
   return launch_rows<8, 2, 2>(a, int8, stream);
 }
 
