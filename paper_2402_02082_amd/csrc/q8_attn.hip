@@ -36,14 +36,15 @@
 //
 // Bound: the memory where keys are long (sixteen sequences of 16 to 32 thousand
 // tokens, 32 heads, five rows: 3.23 GB in 465 us, 6.9 TB/s; the matrix cores busy
-// a tenth of it).  Short ones pay about 10 us around the stream: 2.5 for the launch
-// and finding the run, 2 for the queries and the first blocks, 2 to 4 for ring
-// rows, 1 to 3 for the joins (four sequences of 40 heads, 32 tree rows, 110 MB:
-// 27 us; sixteen sequences, four query heads to each of eight cached ones, 168 MB:
-// 35).  A 7B layer's chain of five behind 512 tokens takes 7.5 us.  64 rows are
-// bound by the conversions, the softmax and the matrix instructions in turn
-// (eight sequences of 52 heads, 64 tree rows: 165 us, 4.1 TB/s, vector
-// instructions 45 % and matrix instructions 23 % of the cycles).
+// a tenth of it).  Short ones take 8 to 9 us more than a plain stream of their
+// bytes: 1.3 until a workgroup knows its run, 2 until queries and first blocks are
+// there, 1 for the join of the waves and as much for their different ends, 1 to
+// count a run in and 2 to 3 to join those of a pair (four sequences of 40 heads, 32
+// tree rows, 110 MB: 26.3 us; sixteen sequences, four query heads to each of eight
+// cached ones, 168 MB: 33.3).  A 7B layer's chain of five behind 512 tokens takes
+// 6.2 us.  64 rows are bound by the conversions, the softmax and the matrix
+// instructions in turn (eight sequences of 52 heads, 64 tree rows: 164 us, 4.1
+// TB/s, vector instructions 45 % and matrix instructions 23 % of the cycles).
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -339,7 +340,7 @@ __device__ __forceinline__ bool find_run(const Q8AttnArgs& a, bool tree, int run
     }
   } else if (a.B == 1) {
     const int units = units_of(a, tree, __builtin_amdgcn_readfirstlane(tokens(a, 0)));
-    const int most = units * a.H_kv >= a.target * a.long_run ? a.target : (a.target + 1) / 2, n = max(1, most / a.H_kv);
+    const int n = max(1, a.target / a.H_kv);
     per = max((units + n - 1) / n, a.min_units);
   } else {
     // about the fewest units a run with which no more than `most` runs come out;
@@ -883,15 +884,19 @@ Q8AttnPlan plan_q8_attn(int B, int N, int H, int H_kv, int n_blocks, int max_spl
   } else {
     // Joining runs takes 3 us, so short pairs are not split, and where workgroups
     // take more than half of the CUs only those that are long for their call are
-    // (one sequence of 32 heads, five rows, 25 units: 7.6 us whole, 8.5 split; of 40
-    // heads, 32 rows: 32 units 12.4 and 13.3, 48 units 15.0 and 14.1).
+    // (one sequence of 32 heads, five rows, 25 units: 7.0 us whole, 8.6 in three runs;
+    // of 40 heads, 32 rows: 32 units 12.4 and 13.7 in two, 48 units 14.9 and 14.0 in
+    // three).
     p.whole_units = few ? (p.waves == 4 ? 28 : 40) : 48;
     p.min_units = p.waves == 4 ? 8 : 16;
-    // Up to one run a CU; of four waves two from 32 units a run on (7B layer of 2048
-    // tokens: 8 runs a pair 10.4 us, 9 14.4; one head group of 60000 tokens, 32
-    // runs a pair 25.7, 63 28.2; 128 pairs of 160 units 36.8 with one, 35.0 with two).
-    p.target = max(1, (p.waves == 4 ? 2 : 1) * kNumCU / p.groups);
-    p.long_run = p.waves == 4 ? 32 : 0;
+    // Up to one run a CU (7B layer of 2048 tokens: 8 runs a pair 9.7 us, 9 11.9; one
+    // head group of 60000 tokens, 32 runs a pair 25.1, 63 27.7); of four waves and
+    // sequences that may differ in length two, from 32 units a run on (sixteen
+    // sequences of 64 to 256 units, 8 heads: 33.1 us, with one run a CU 34.4; where
+    // all are 160 long 32.6 and 30.9).
+    const bool two = p.waves == 4 && B > 1;
+    p.target = max(1, (two ? 2 : 1) * kNumCU / p.groups);
+    p.long_run = two ? 32 : 0;
     p.runs = max(pairs, min(pairs + p.target, pairs * ((most + p.min_units - 1) / p.min_units)));
     if (most <= p.whole_units) return p;  // no pair will be split: no states
   }
