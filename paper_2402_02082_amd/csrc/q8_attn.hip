@@ -6,7 +6,7 @@
 // behind them and for the tree.
 //
 // Work decomposition.  The query rows of a cached head (N rows of each of the
-// H / H_kv query heads that share it) are cut into groups of up to 64, its keys
+// H / H_kv query heads that share it) are cut into groups of up to 32, its keys
 // into units of 32 tokens: the whole blocks, then the ring's rows.  Each pair
 // (sequence, cached head) is split into as many runs of units as its length
 // asks for, so that all runs of a call are of about the same size whatever the
@@ -14,10 +14,10 @@
 // there; of the others each run leaves a state, counts itself in, and the one
 // that completes the pair joins the states in order, whichever that is: one
 // launch.
-// A workgroup's waves (eight, or four for few pairs of few rows) take units in turn,
-// each for all of the group's rows (up to 32 rows; 64 rows: four waves for each
-// half, the second read of a unit then comes from L2), so each code is converted
-// by one or two waves.
+// A workgroup's waves (eight or four) take units in turn, each for all of the
+// group's rows.  Groups of one run lie on the same XCD, so that all but one of them
+// read its keys from L2 (64 rows in one workgroup instead, four waves for each half:
+// 166 us where two groups take 147, 622 and 470 for long contexts).
 //
 // Per unit and wave, on v_mfma_f32_16x16x32:
 //   S^T[key, query] = K Q^T, softmax on S^T with one query per lane column,
@@ -42,9 +42,9 @@
 // count a run in and 2 to 3 to join those of a pair (four sequences of 40 heads, 32
 // tree rows, 110 MB: 26.3 us; sixteen sequences, four query heads to each of eight
 // cached ones, 168 MB: 33.3).  A 7B layer's chain of five behind 512 tokens takes
-// 6.2 us.  64 rows are bound by the conversions, the softmax and the matrix
-// instructions in turn (eight sequences of 52 heads, 64 tree rows: 164 us, 4.1
-// TB/s, vector instructions 45 % and matrix instructions 23 % of the cycles).
+// 6.2 us.  Several groups of rows are bound by the conversions, the softmax and the
+// matrix instructions in turn (eight sequences of 52 heads, 64 tree rows, 677 MB:
+// 146 us, 4.6 TB/s).
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -411,12 +411,12 @@ struct JoinLds {
 // 1 / sum of a row's probabilities; 0 where it saw no key, and NaN stays.
 __device__ __forceinline__ float reciprocal(float l) { return l > 0.f ? __builtin_amdgcn_rcpf(l) : (l == 0.f ? 0.f : l); }
 
-// Maximum and sum of a row over a group's key waves.
+// Maximum and sum of a row over the waves.
 template <int WAVES, class Lds>
-__device__ __forceinline__ void join_sums(const Lds& lds, int first, int row, float& M, float& L) {
+__device__ __forceinline__ void join_sums(const Lds& lds, int row, float& M, float& L) {
   float m[WAVES], l[WAVES];
 #pragma unroll
-  for (int w = 0; w < WAVES; ++w) m[w] = lds.m[first + w][row], l[w] = lds.l[first + w][row];
+  for (int w = 0; w < WAVES; ++w) m[w] = lds.m[w][row], l[w] = lds.l[w][row];
   M = m[0];
 #pragma unroll
   for (int w = 1; w < WAVES; ++w) M = fmaxf(M, m[w]);
@@ -503,23 +503,22 @@ __device__ __forceinline__ void join_states(const Q8AttnArgs& a, int first, int 
   }
 }
 
-template <int WAVES, int NT, int RG, bool INT8, bool TREE>
+// SHARED: several groups read the same keys.
+template <int WAVES, int NT, bool SHARED, bool INT8, bool TREE>
 __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2)))
 void q8_attn_kernel(Q8AttnArgs a) {
   constexpr int kThreads = 64 * WAVES;
-  constexpr int kKeyWaves = WAVES / RG;
   constexpr int kStages = NT == 1 ? 2 : 1;
-  constexpr int kPolicy = RG == 1 ? kStream : kKeep;
-  constexpr int kRows = 16 * NT * RG;  // query rows of a workgroup
+  constexpr int kPolicy = SHARED ? kKeep : kStream;
+  constexpr int kRows = 16 * NT;  // query rows of a workgroup
   const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int kw = wave % kKeyWaves, rg = wave / kKeyWaves;
   // Workgroups go to the eight XCDs in turn; the groups of a run are eight
   // apart, on the same XCD and so on the same L2, which they share its keys in.
   const int grp = a.groups == 1 ? 0 : blockIdx.x / 8 % a.groups;
   const int run = a.groups == 1 ? blockIdx.x : blockIdx.x / (8 * a.groups) * 8 + blockIdx.x % 8;
-  const int G = a.G, R = a.N * G, row0 = grp * kRows + rg * 16 * NT;
-  __shared__ JoinLds<WAVES, 16 * NT> lds;
+  const int G = a.G, R = a.N * G, row0 = grp * kRows;
+  __shared__ JoinLds<WAVES, kRows> lds;
 
   // Query rows: row r is node r / G of query head hk * G + r % G.  MFMA step
   // 2 h + e holds dims 64 h + 16 g + 8 e + (0..7).  A single sequence's are
@@ -551,17 +550,17 @@ void q8_attn_kernel(Q8AttnArgs a) {
   const uint8_t* blocks = a.cache.blocks + head * a.n_blocks * (size_t)kQ8BlockBytes;
   const float* scales = a.cache.scales + head * a.n_blocks * 2;
 
-  // The run's units among its key waves.  The last waves take one ring unit each
+  // The run's units among the waves.  The last waves take one ring unit each
   // (a ring holds at most 95 rows, three units); the blocks go in turn, but that
   // waves without a ring unit take kRingCost of them before.
-  static_assert(kKeyWaves > 3, "a ring unit a wave");
+  static_assert(WAVES > 3, "a ring unit a wave");
   const int ue = min(u1, whole), ring_units = max(0, u1 - max(u0, whole));
-  const bool ring = kw >= kKeyWaves - ring_units;
-  const int early_waves = ring_units ? kKeyWaves - ring_units : 0, turns = u0 + early_waves * kRingCost;
-  int u = early_waves && !ring ? u0 + kw : turns + kw;
+  const bool ring = wave >= WAVES - ring_units;
+  const int early_waves = ring_units ? WAVES - ring_units : 0, turns = u0 + early_waves * kRingCost;
+  int u = early_waves && !ring ? u0 + wave : turns + wave;
   auto next = [&](int at) {
     const int more = at + early_waves;
-    return at >= turns ? at + kKeyWaves : (more < turns ? more : turns + kw);
+    return at >= turns ? at + WAVES : (more < turns ? more : turns + wave);
   };
   RawUnit raw[kStages];
   float2 unit_scale[kStages];  // of K, of V
@@ -578,7 +577,7 @@ void q8_attn_kernel(Q8AttnArgs a) {
   };
   if (a.B > 1) load_queries(b, hk);
 
-  const int j0 = (max(u0, whole) + kKeyWaves - 1 - kw) * kQ8Block;  // the ring unit's first token
+  const int j0 = (max(u0, whole) + WAVES - 1 - wave) * kQ8Block;  // the ring unit's first token
   int parent = -1;
   u32x4_t kf[2][4], v[8];
   auto load_ring = [&] {
@@ -790,7 +789,7 @@ void q8_attn_kernel(Q8AttnArgs a) {
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
     float M, Lsum;
-    join_sums<kKeyWaves>(lds, rg * kKeyWaves, 16 * nt + c, M, Lsum);
+    join_sums<WAVES>(lds, 16 * nt + c, M, Lsum);
     const float part = (sm[nt].m == neg_inf() ? 0.f : fast_exp2(sm[nt].m - M)) * reciprocal(Lsum);
     const float unit = sm[nt].lc == kNoFactor ? 0.f : fast_exp2(-sm[nt].lc);
 #pragma unroll
@@ -807,14 +806,13 @@ void q8_attn_kernel(Q8AttnArgs a) {
   {
     constexpr int kTPR = kThreads / kRows, kDims = kD / kTPR;  // threads a row, dims a thread
     const int in = tid / kTPR, d = tid % kTPR * kDims, r = grp * kRows + in;
-    const int first = in / (16 * NT) * kKeyWaves, row = in % (16 * NT);
     f32x4_t o[kDims / 4];
 #pragma unroll
     for (int i = 0; i < kDims / 4; ++i) o[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int w = 0; w < kKeyWaves; ++w)
+    for (int w = 0; w < WAVES; ++w)
 #pragma unroll
-      for (int i = 0; i < kDims / 4; ++i) o[i] += *(const f32x4_t*)&lds.o[first + w][row][d + 4 * i];
+      for (int i = 0; i < kDims / 4; ++i) o[i] += *(const f32x4_t*)&lds.o[w][in][d + 4 * i];
     if (r < R && finished) {
       const int n = r / G;
       uint16_t* dst = a.out + (((size_t)b * a.N + n) * a.H + hk * G + (r - n * G)) * kD + d;
@@ -825,7 +823,7 @@ void q8_attn_kernel(Q8AttnArgs a) {
       const size_t at = ((size_t)run * a.groups + grp) * kRows;
       if (d == 0) {
         float M, Lsum;
-        join_sums<kKeyWaves>(lds, first, row, M, Lsum);
+        join_sums<WAVES>(lds, in, M, Lsum);
         __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2_t, f32x2_t{M, Lsum}),
                                               state_rsrc(a.part_ml + at, kRows * 8), in * 8, 0, kDeviceScope);
       }
@@ -843,18 +841,18 @@ void q8_attn_kernel(Q8AttnArgs a) {
                        a.out + ((size_t)b * a.N * a.H + hk * G) * kD, grp * kRows, G, lds);
 }
 
-template <int WAVES, int NT, int RG>
+template <int WAVES, int NT, bool SHARED>
 hipError_t launch_rows(const Q8AttnArgs& a, bool int8, hipStream_t stream) {
   const long runs = a.groups == 1 ? a.runs : (a.runs + 7) / 8 * 8;
   const dim3 grid((unsigned)(runs * a.groups)), block(64 * WAVES);
   if (a.parents && int8)
-    hipLaunchKernelGGL((q8_attn_kernel<WAVES, NT, RG, true, true>), grid, block, 0, stream, a);
+    hipLaunchKernelGGL((q8_attn_kernel<WAVES, NT, SHARED, true, true>), grid, block, 0, stream, a);
   else if (a.parents)
-    hipLaunchKernelGGL((q8_attn_kernel<WAVES, NT, RG, false, true>), grid, block, 0, stream, a);
+    hipLaunchKernelGGL((q8_attn_kernel<WAVES, NT, SHARED, false, true>), grid, block, 0, stream, a);
   else if (int8)
-    hipLaunchKernelGGL((q8_attn_kernel<WAVES, NT, RG, true, false>), grid, block, 0, stream, a);
+    hipLaunchKernelGGL((q8_attn_kernel<WAVES, NT, SHARED, true, false>), grid, block, 0, stream, a);
   else
-    hipLaunchKernelGGL((q8_attn_kernel<WAVES, NT, RG, false, false>), grid, block, 0, stream, a);
+    hipLaunchKernelGGL((q8_attn_kernel<WAVES, NT, SHARED, false, false>), grid, block, 0, stream, a);
   return hipGetLastError();
 }
 
@@ -863,13 +861,18 @@ hipError_t launch_rows(const Q8AttnArgs& a, bool int8, hipStream_t stream) {
 Q8AttnPlan plan_q8_attn(int B, int N, int H, int H_kv, int n_blocks, int max_splits) {
   Q8AttnPlan p{};
   const int R = N * (H / H_kv);
-  p.rows = R <= 16 ? 16 : (R <= 32 ? 32 : 64);
+  p.rows = R <= 16 ? 16 : 32;
   p.groups = (R + p.rows - 1) / p.rows;
   p.waves = 8;
   const long pairs = (long)B * H_kv, most = n_blocks + (kQ8Block - 1 + N + kQ8Block - 1) / kQ8Block;
   const long wgs = pairs * p.groups;  // one a pair and group
   // Enough for every CU: nothing is split (nor past the counters).
   if (max_splits == 1 || most == 1 || wgs > (max_splits ? kCounterSlots : kNumCU - 1)) {
+    // Several groups of more workgroups than CUs: four waves, two a CU (8 sequences
+    // of 52 heads, 64 rows: 147 us, with eight waves 158; 16 of 8 heads, 128 pairs of
+    // two groups: 57.5 and 46.8).  One group reads each key once and keeps eight
+    // (8 sequences of 40 heads, 32 rows: 41.3 us, with four 44.9).
+    if (p.groups > 1 && wgs > kNumCU) p.waves = 4;
     p.splits = 1;
     p.runs = pairs;
     return p;
@@ -908,9 +911,9 @@ Q8AttnPlan plan_q8_attn(int B, int N, int H, int H_kv, int n_blocks, int max_spl
 }
 
 hipError_t launch_q8_attn(const Q8AttnArgs& a, bool int8, int rows, int waves, hipStream_t stream) {
-  if (rows == 16) return waves == 4 ? launch_rows<4, 1, 1>(a, int8, stream) : launch_rows<8, 1, 1>(a, int8, stream);
-  if (rows == 32) return launch_rows<8, 2, 1>(a, int8, stream);
-  return launch_rows<8, 2, 2>(a, int8, stream);
+  if (rows == 16) return waves == 4 ? launch_rows<4, 1, false>(a, int8, stream) : launch_rows<8, 1, false>(a, int8, stream);
+  if (a.groups == 1) return launch_rows<8, 2, false>(a, int8, stream);
+  return waves == 4 ? launch_rows<4, 2, true>(a, int8, stream) : launch_rows<8, 2, true>(a, int8, stream);
 }
 
 }  // namespace glide
