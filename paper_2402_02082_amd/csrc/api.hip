@@ -203,7 +203,8 @@ int q8_lens_check(const int32_t* seq_lens, const int32_t* more, int fixed, int m
 bool q8_attn_sizes_ok(int B, int N, int H, int H_kv, int D, int L_cap) {
   if (!q8_sizes_ok(B, H_kv, D, L_cap, GLIDE_E4M3)) return false;
   if (N < 1 || N > glide::kMaxNodes || H < H_kv || H % H_kv) return false;
-  // with that, at most 2^21 + 2^22 workgroups of 512 threads: a grid's 2^32
+  // with that, at most 2^21 workgroups of 512 threads, or of several groups of 32
+  // rows a pair 2^21 + 2^23 of 256: a grid's 2^32
   return (double)B * N * H < (1 << 28);
 }
 

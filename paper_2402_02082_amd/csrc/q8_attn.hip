@@ -513,10 +513,15 @@ void q8_attn_kernel(Q8AttnArgs a) {
   constexpr int kRows = 16 * NT;  // query rows of a workgroup
   const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  // Workgroups go to the eight XCDs in turn; the groups of a run are eight
-  // apart, on the same XCD and so on the same L2, which they share its keys in.
-  const int grp = a.groups == 1 ? 0 : blockIdx.x / 8 % a.groups;
-  const int run = a.groups == 1 ? blockIdx.x : blockIdx.x / (8 * a.groups) * 8 + blockIdx.x % 8;
+  // Workgroups go to the eight XCDs in turn; the groups of a run are eight apart, on
+  // the same XCD and so on the same L2, which they share its keys in.  The last
+  // runs, fewer than eight, have their groups on all XCDs.
+  int grp = 0, run = blockIdx.x;
+  if (SHARED) {
+    const int even = a.runs / 8 * 8, id = blockIdx.x, rest = id - even * a.groups;
+    grp = rest < 0 ? id / 8 % a.groups : rest / (a.runs - even);
+    run = rest < 0 ? id / (8 * a.groups) * 8 + id % 8 : even + rest % (a.runs - even);
+  }
   const int G = a.G, R = a.N * G, row0 = grp * kRows;
   __shared__ JoinLds<WAVES, kRows> lds;
 
@@ -843,8 +848,7 @@ void q8_attn_kernel(Q8AttnArgs a) {
 
 template <int WAVES, int NT, bool SHARED>
 hipError_t launch_rows(const Q8AttnArgs& a, bool int8, hipStream_t stream) {
-  const long runs = a.groups == 1 ? a.runs : (a.runs + 7) / 8 * 8;
-  const dim3 grid((unsigned)(runs * a.groups)), block(64 * WAVES);
+  const dim3 grid((unsigned)((long)a.runs * a.groups)), block(64 * WAVES);
   if (a.parents && int8)
     hipLaunchKernelGGL((q8_attn_kernel<WAVES, NT, SHARED, true, true>), grid, block, 0, stream, a);
   else if (a.parents)

@@ -169,6 +169,23 @@ def test_plans(B, H, Hk, N, top):
         assert torch.equal(run(q, cache, lens, par), out)
 
 
+@pytest.mark.parametrize("B,H,Hk,N", [(1, 60, 1, 64), (2, 88, 1, 64), (11, 24, 1, 64), (5, 12, 2, 50)])
+def test_few_pairs_of_many_query_rows(B, H, Hk, N):
+    """One or a few cached heads for all query heads: the groups of runs that do not
+    fill the eight XCDs' turns are spread over all of them."""
+    require_gpu()
+    say("groups", B, H, Hk, N)
+    rng = np.random.default_rng(H)
+    lens = [int(x) for x in rng.integers(1, 500, B)]
+    cache, k, v = fill(B, Hk, lens, "e4m3", 56)
+    tk, tv = rows((B, N, Hk, 128), 57), rows((B, N, Hk, 128), 58)
+    glide.glide_q8_append(tk, tv, cache, ints(lens), hold=True)
+    q, par = cpu_normal((B, N, H, 128), 59, BF).cuda(), [random_tree(N, rng) for _ in range(B)]
+    for splits in (0, 1, 3):
+        out = run(q, cache, lens, par, max_splits=splits)
+        check(out, q, k, v, lens, "e4m3", tk, tv, par, nodes=[0, N // 2, N - 1])
+
+
 @pytest.mark.parametrize("pairs", [4, 140])
 @pytest.mark.parametrize("N", [3, 7, 10, 13])
 def test_rows_that_do_not_fill_the_waves(pairs, N):
