@@ -665,6 +665,7 @@ int glide_q8_tree_attn(const void* q, const glide_q8_cache* cache, const int32_t
   a.min_units = p.min_units;
   a.whole_units = p.whole_units;
   a.long_run = p.long_run;
+  a.join_ratio = p.join_ratio;
   a.runs = (int)p.runs;
   const double sc = scale > 0.f ? (double)scale : 1.0 / sqrt((double)D);
   a.scale_log2 = (float)(sc * 1.4426950408889634);  // log2(e)

@@ -81,9 +81,11 @@ hipError_t launch_q8_commit(const Q8CommitArgs& a, bool int8, hipStream_t stream
 // keys in runs of units -- `splits` of every pair (sequence, cached head), or
 // with splits == 0 up to `target` (half of it if they would be shorter than
 // long_run units then) of about equal size in all, of at least min_units units
-// each, and pairs of up to whole_units in one.  runs: at most so many.
+// each, pairs of up to whole_units in one, and no more runs of a pair than the root
+// of its units times join_ratio.  runs: at most so many.
 struct Q8AttnPlan {
   int rows, groups, waves, splits, target, min_units, whole_units, long_run;
+  float join_ratio;
   long runs;
   size_t ws_bytes, part_ml_off, part_o_off;
 };
@@ -100,7 +102,7 @@ struct Q8AttnArgs {
   float2* part_ml;  // [runs, groups, rows]: (max in log2 units, sum)
   int B, N, H, H_kv, G, n_blocks, groups, splits,  // G: query heads a cached one
       target, min_units, whole_units, long_run, runs;
-  float scale_log2;
+  float join_ratio, scale_log2;
 };
 hipError_t launch_q8_attn(const Q8AttnArgs& a, bool int8, int rows, int waves, hipStream_t stream);
 
