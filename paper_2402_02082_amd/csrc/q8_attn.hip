@@ -17,7 +17,7 @@
 // A workgroup's waves (eight or four) take units in turn, each for all of the
 // group's rows.  Groups of one run lie on the same XCD, so that all but one of them
 // read its keys from L2 (64 rows in one workgroup instead, four waves for each half:
-// 166 us where two groups take 147, 622 and 470 for long contexts).
+// 166 us where two groups take 145, 622 and 454 for long contexts).
 //
 // Per unit and wave, on v_mfma_f32_16x16x32:
 //   S^T[key, query] = K Q^T, softmax on S^T with one query per lane column,
@@ -36,15 +36,17 @@
 //
 // Bound: the memory where keys are long (sixteen sequences of 16 to 32 thousand
 // tokens, 32 heads, five rows: 3.23 GB in 465 us, 6.9 TB/s; the matrix cores busy
-// a tenth of it).  Short ones take 8 to 9 us more than a plain stream of their
+// a tenth of it).  Short ones take 7 to 9 us more than a plain stream of their
 // bytes: 1.3 until a workgroup knows its run, 2 until queries and first blocks are
 // there, 1 for the join of the waves and as much for their different ends, 1 to
-// count a run in and 2 to 3 to join those of a pair (four sequences of 40 heads, 32
-// tree rows, 110 MB: 26.3 us; sixteen sequences, four query heads to each of eight
-// cached ones, 168 MB: 33.3).  A 7B layer's chain of five behind 512 tokens takes
-// 6.2 us.  Several groups of rows are bound by the conversions, the softmax and the
-// matrix instructions in turn (eight sequences of 52 heads, 64 tree rows, 677 MB:
-// 146 us, 4.6 TB/s).
+// count a run in and 2 to join those of a pair (four sequences of 40 heads, 32 tree
+// rows, 110 MB: 25.4 us; sixteen sequences, four query heads to each of eight
+// cached ones, 168 MB: 32.4).  A 7B layer's chain of five behind 512 tokens takes
+// 6.1 us.  Code that runs once costs as much as the trips to memory it waits for:
+// what is rare stands apart, and little is unrolled outside the loop over blocks.
+// Several groups of rows are bound by the conversions, the softmax and the matrix
+// instructions in turn (eight sequences of 52 heads, 64 tree rows, 677 MB: 145 us,
+// 4.7 TB/s).
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -898,8 +900,8 @@ Q8AttnPlan plan_q8_attn(int B, int N, int H, int H_kv, int n_blocks, int max_spl
   // Enough for every CU: nothing is split (nor past the counters).
   if (max_splits == 1 || most == 1 || wgs > (max_splits ? kCounterSlots : kNumCU - 1)) {
     // Several groups of more workgroups than CUs: four waves, two a CU (8 sequences
-    // of 52 heads, 64 rows: 147 us, with eight waves 158; 16 of 8 heads, 128 pairs of
-    // two groups: 57.5 and 46.8).  One group reads each key once and keeps eight
+    // of 52 heads, 64 rows: 145 us, with eight waves 158; 16 of 8 heads, 128 pairs of
+    // two groups: 57.5 and 45.8).  One group reads each key once and keeps eight
     // (8 sequences of 40 heads, 32 rows: 41.3 us, with four 44.9).
     if (p.groups > 1 && wgs > kNumCU) p.waves = 4;
     p.splits = 1;
@@ -916,21 +918,21 @@ Q8AttnPlan plan_q8_attn(int B, int N, int H, int H_kv, int n_blocks, int max_spl
   } else {
     // Joining runs takes 3 us, so short pairs are not split, and where workgroups
     // take more than half of the CUs only those that are long for their call are
-    // (one sequence of 32 heads, five rows, 25 units: 7.0 us whole, 8.6 in three runs;
-    // of 40 heads, 32 rows: 32 units 12.4 and 13.7 in two, 48 units 14.9 and 14.0 in
+    // (one sequence of 32 heads, five rows, 25 units: 6.9 us whole, 8.0 in three runs;
+    // of 40 heads, 32 rows: 32 units 12.3 and 12.9 in two, 48 units 14.8 and 13.2 in
     // three).
     p.whole_units = few ? (p.waves == 4 ? 28 : 40) : 48;
     p.min_units = p.waves == 4 ? 8 : 16;
-    // Up to one run a CU (7B layer of 2048 tokens: 8 runs a pair 9.7 us, 9 11.9; one
-    // head group of 60000 tokens, 32 runs a pair 25.1, 63 27.7); of four waves and
+    // Up to one run a CU (7B layer of 2048 tokens: 8 runs a pair 9.3 us, 9 11.1; one
+    // head group of 60000 tokens, 32 runs a pair 24.5, 63 26.6); of four waves and
     // sequences that may differ in length two, from 32 units a run on (sixteen
     // sequences of 64 to 256 units, 8 heads: 33.1 us, with one run a CU 34.4; where
-    // all are 160 long 32.6 and 30.9).
+    // all are 160 long 32.3 and 31.5).
     const bool two = p.waves == 4 && B > 1;
     p.target = max(1, (two ? 2 : 1) * kNumCU / p.groups);
     p.long_run = two ? 32 : 0;
     // One pair of 16000 tokens, 32 rows: 12 to 16 runs 18.8 us, 32 21.4; of 60000
-    // 32 runs 27.2, 64 33.0; one row of 30000 tokens 32 runs 13.8, 64 16.0.
+    // 32 runs 27.2, 64 33.0; one row of 30000 tokens 32 runs 12.8, 64 13.5, 128 17.7.
     p.join_ratio = p.waves == 4 ? 2.5f : 0.5f;
     p.runs = max(pairs, min(pairs + p.target, pairs * ((most + p.min_units - 1) / p.min_units)));
     if (most <= p.whole_units) return p;  // no pair will be split: no states
