@@ -183,8 +183,16 @@ __device__ __forceinline__ void softmax_unit(float (&x)[8], RowState& st, f32x4_
     if (st.m != neg_inf()) {
       st.l *= fast_exp2(st.m - m_new);
       if (st.lc != kNoFactor) {
-        st.lc = fminf(st.lc + (m_new - st.m), kFactorMost);
+        // c grows as the weights of earlier keys fall, and the accumulators stay;
+        // where it would pass its most (values below about 2^-100) they fall
+        const float lc = st.lc + (m_new - st.m);
+        st.lc = fminf(lc, kFactorMost);
         st.c = fast_exp2(st.lc);
+        if (lc > kFactorMost) {
+          const float r = fast_exp2(kFactorMost - lc);
+#pragma unroll
+          for (int t = 0; t < 8; ++t) acc[t] *= r;
+        }
       }
     }
     st.m = m_new;

@@ -1,0 +1,104 @@
+"""Attention over the 8-bit cache where values are as small as bfloat16 has them,
+on the GPU against the float64 oracle: a wave sees several units whose scores
+rise, so that the maximum, the factor of the products and what is summed so far
+move together.
+
+Tolerance, beside the terms derived in test_gpu_q8_attn.py (the same here):
+* the factor c is at most 2^126, so a product p * s * c of a block whose scale s
+  is small lies below fp16's normal numbers and is off by half their step, 2^-25;
+  over c, and times a code of at most 448, that is 448 * 2^-151 < 2^-142 a key;
+* c is held as its log2, a float32 below 128 whose steps are 2^-17: each time it
+  moves, what was summed is off by 2^-18 of it and the power by about as much.
+  A wave moves it once a unit at most, 24 here: 2^-13 of the average magnitude."""
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2402_02082_amd as glide
+from oracle import attention as OA
+from oracle import q8 as OQ
+from tests.gpu_common import cpu_normal, require_gpu, say
+from tests.test_gpu_q8_attn import random_tree, run
+from tests.test_gpu_q8_cache import KINDS, f64, ints, junk_cache, rows
+
+pytestmark = pytest.mark.gpu
+
+BF, F32 = torch.bfloat16, torch.float32
+
+
+def check(got, q, k, v, L, kind, tk=None, tv=None, par=None):
+    """One sequence: got, q [1, N, H, 128], k, v [1, L, H, 128]."""
+    got, q = f64(got)[0], f64(q)[0]
+    for j in range(k.shape[2]):
+        ks, vs = (OQ.stored(f64(x[0, :L, j]), kind) for x in (k, v))
+        for n in range(q.shape[0]):
+            kk, vv = ks, vs
+            if par is not None:
+                own = OA.ancestor_or_self(par, n)
+                kk, vv = np.concatenate([ks, f64(tk[0, own, j])]), np.concatenate([vs, f64(tv[0, own, j])])
+            row, keys, sc = q[n, j:j + 1], len(kk), 1 / np.sqrt(128)
+            want, A = OA.attention_rows(row, kk, vv, sc), OA.attention_rows(row, kk, np.abs(vv), sc)
+            score = np.linalg.norm(row) * np.linalg.norm(kk, axis=1).max() * sc
+            rel = 2.0 ** -11 + 2.0 ** -13 + 2 * keys * 2.0 ** -24 + 2 * 131 * 2.0 ** -24 * score
+            tol = (2.0 ** -8 * np.abs(want) + rel * A + keys * (2.0 ** -32 * np.abs(vv).max() + 2.0 ** -142)
+                   + 2.0 ** -134)
+            err = np.abs(got[n, j:j + 1] - want)
+            assert np.all(err <= tol), (j, n, float((err / tol).max()), float(np.abs(want).max()))
+
+
+def _order(order, blocks):
+    if order == "rise":
+        return np.arange(blocks)
+    if order == "fall":
+        return np.arange(blocks)[::-1]
+    return np.random.default_rng(1).permutation(blocks)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("order", ["rise", "fall", "mixed"])
+@pytest.mark.parametrize("N", [4, 20])
+def test_scores_that_rise_from_block_to_block(kind, order, N):
+    """The scores of a block and the next differ by about 3 (in log2), so those of a
+    wave's units by 12 to 24, and what came before has next to no weight behind
+    them; blocks and ring rows, one run a pair and several."""
+    require_gpu()
+    H, L = 2, 32 * 23 + 20
+    d = cpu_normal((1, 1, H, 128), 1, F32)
+    d = d / d.pow(2).sum(-1, keepdim=True).sqrt() * 128 ** 0.5
+    step = torch.from_numpy(_order(order, 24).repeat(32)[:L].copy()).float()[None, :, None, None]
+    k = (d * (0.25 * step) + 0.1 * cpu_normal((1, L, H, 128), 2, F32)).to(BF).cuda()
+    # |d|^2 / sqrt(128) = 11.3, times log2(e): a step of 0.25 is 4.1 for a query of d
+    q = (d * torch.linspace(0.6, 1.0, N)[None, :, None, None]).to(BF).cuda()
+    v0 = cpu_normal((1, L, H, 128), 3, F32).clamp(-3, 3)
+    tk, tv0 = (d * 3.0).expand(1, N, H, 128).contiguous().to(BF).cuda(), cpu_normal((1, N, H, 128), 4, F32).clamp(-3, 3)
+    par = random_tree(N, np.random.default_rng(N))
+    for size in (1e-36, 1e-35, 1e-34, 1e-33, 1e-31, 1e-28, 1.0):
+        v, tv = ((x.double() * size).to(BF).cuda() for x in (v0, tv0))
+        cache = junk_cache(1, H, L + 1, kind)
+        glide.glide_q8_append(k, v, cache, ints([0]))
+        for splits in (1, 0, 3):
+            say("rising scores", kind, order, N, size, splits)
+            check(run(q, cache, [L], max_splits=splits), q, k, v, L, kind)
+        glide.glide_q8_append(tk, tv, cache, ints([L]), hold=True)
+        check(run(q, cache, [L], [par], max_splits=1), q, k, v, L, kind, tk, tv, par)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_peaked_scores_of_small_values(kind):
+    """Queries times 24 against keys of ordinary size."""
+    require_gpu()
+    H, L = 2, 700
+    k, v0 = rows((1, L, H, 128), 5, spread=False), rows((1, L, H, 128), 6, spread=False)
+    for N in (3, 20, 50):
+        q = (cpu_normal((1, N, H, 128), 7, F32) * 24).to(BF).cuda()
+        tk, tv0 = rows((1, N, H, 128), 8, spread=False), rows((1, N, H, 128), 9, spread=False)
+        par = random_tree(N, np.random.default_rng(N))
+        for size in (1e-36, 1e-34, 1e-33, 1e-31):
+            v, tv = ((x.double() * size).to(BF) for x in (v0, tv0))
+            cache = junk_cache(1, H, L + 1, kind)
+            glide.glide_q8_append(k, v, cache, ints([0]))
+            glide.glide_q8_append(tk, tv, cache, ints([L]), hold=True)
+            for splits in (1, 0):
+                say("peaked", kind, N, size, splits)
+                check(run(q, cache, [L], [par], max_splits=splits), q, k, v, L, kind, tk, tv, par)
