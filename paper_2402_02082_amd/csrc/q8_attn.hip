@@ -671,7 +671,9 @@ void q8_attn_kernel(Q8AttnArgs a) {
           top = max(top, max(lo < 0x7f80u ? lo : 0u, hi < 0x7f80u ? hi : 0u));
         }
     }
+    // (the logarithm takes a subnormal number for zero, so they count as the least normal one)
     top = wave_max(top);
+    if (top != 0) top = max(top, 0x80u);
     const float ls = __builtin_amdgcn_logf(__uint_as_float(top << 16)) - 8.f;  // as if the largest were a code of 256
     uint64_t mine = 0;  // ancestor mask of node `lane`
     if (TREE) mine = ancestor_mask(lane < a.N ? parent : -1, lane);

@@ -102,3 +102,24 @@ def test_peaked_scores_of_small_values(kind):
             for splits in (1, 0):
                 say("peaked", kind, N, size, splits)
                 check(run(q, cache, [L], [par], max_splits=splits), q, k, v, L, kind, tk, tv, par)
+
+
+def test_ring_rows_of_subnormal_values():
+    """Rows behind the last whole block whose values are all below 2^-126, alone and
+    behind blocks of zeros (a block of such values is one of zeros)."""
+    require_gpu()
+    for L in (0, 20, 84):
+        for N in (3, 20):
+            say("subnormal", L, N)
+            H = 2
+            n = max(L, 1)
+            k, v = rows((1, n, H, 128), 10, spread=False), rows((1, n, H, 128), 11, spread=False).double()
+            v = (v.clamp(-3, 3) * 2.0 ** -129).to(BF)
+            tk, tv = rows((1, N, H, 128), 12, spread=False), rows((1, N, H, 128), 13, spread=False).double()
+            tv = (tv.clamp(-3, 3) * 2.0 ** -129).to(BF)
+            cache = junk_cache(1, H, 128, "e4m3")
+            glide.glide_q8_append(k, v, cache, ints([0]), ints([L]))
+            glide.glide_q8_append(tk, tv, cache, ints([L]), hold=True)
+            par = random_tree(N, np.random.default_rng(N))
+            q = cpu_normal((1, N, H, 128), 14, BF).cuda()
+            check(run(q, cache, [L], [par]), q, k, v, L, "e4m3", tk, tv, par)
