@@ -451,7 +451,7 @@ typedef struct glide_rope_rows {
  *             number of node t's ancestors if tree_parents [B, T] is given:
  *             the positions of a tree behind a prefix of seq_lens[b] tokens.
  *   D == 128; 2 <= rot_dim <= D, even; 1 <= T <= 4194304 (tree: <= 64);
- *   1 <= B <= 65535; H >= 1; B * T * (q->H + k->H) < 2^31;
+ *   1 <= B <= 65535; H >= 1; q->H + k->H <= 2^26; B * T * (q->H + k->H) < 2^31;
  *   dtype     GLIDE_BF16 or GLIDE_F32 (rows; arithmetic in float32, the angle
  *             reduced in float64).
  */

@@ -517,7 +517,9 @@ int glide_rope(const glide_rope_rows* q, const glide_rope_rows* k, const double*
   if (flags & ~(GLIDE_ROPE_INTERLEAVED | GLIDE_ROPE_BACKWARD)) return GLIDE_EINVAL;
   if (positions && (seq_lens || tree_parents)) return GLIDE_EINVAL;
   if (tree_parents && T > glide::kMaxNodes) return GLIDE_EINVAL;
-  if ((double)B * T * ((double)q->H + (k ? k->H : 0)) > 2147483647.0) return GLIDE_EINVAL;
+  const int64_t heads = (int64_t)q->H + (k ? k->H : 0);
+  if (heads > 1 << 26) return GLIDE_EINVAL;  // up to 16 pieces of each, counted in an int
+  if ((double)B * T * heads > 2147483647.0) return GLIDE_EINVAL;
   if (validate_enabled() && tree_parents) {
     int status = GLIDE_OK;
     std::vector<int32_t> par;

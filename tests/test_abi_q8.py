@@ -204,3 +204,11 @@ def test_binding_rejects_host_tensors():
     for bad in (dict(kind="fp8"), dict(B=0), dict(H_kv=0), dict(L_cap=0)):
         with pytest.raises(ValueError):
             glide.q8_cache(**{**dict(B=1, H_kv=1, L_cap=32, device="cpu"), **bad})
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("H,Hkv", [(1 << 27, 1), (1 << 28, 1), (1, 1 << 27), ((1 << 26), 1), (1, 1 << 26),
+                                   ((1 << 31) - 2, 1)])
+def test_rope_rejects_heads_whose_pieces_pass_an_int(lib, dtype, H, Hkv):
+    """A row is 8 or 16 pieces for the threads of its token, counted in 32 bits."""
+    assert _rope(lib, H=H, Hkv=Hkv, B=1, T=1, dtype=dtype) == EINVAL
