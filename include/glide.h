@@ -578,7 +578,8 @@ int glide_q8_tree_attn(const void* q, const glide_q8_cache* cache, const int32_t
  *   accept_len [B] int32 (clamped to [0, N]); path [B, N] int32 as
  *              glide_verify_commit gives it (with layers == 0 there), or NULL:
  *              the nodes are a chain, 0, 1, ... (spec_sample_verify).
- *   seq_lens_out [B] int32 out (must not be seq_lens).
+ *   seq_lens_out [B] int32 out (sharing no memory with seq_lens, accept_len or
+ *              path).
  *   1 <= N <= 64.  One launch.
  */
 int glide_q8_commit(const glide_q8_cache* caches, int layers, const int32_t* seq_lens,

@@ -186,6 +186,12 @@ bool q8_cache_ok(const glide_q8_cache* c, glide::Q8Cache* out) {
   return true;
 }
 
+// Whether n ints at a and m ints at b share memory.
+bool overlap(const int32_t* a, size_t n, const int32_t* b, size_t m) {
+  const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+  return x < y + m * sizeof(int32_t) && y < x + n * sizeof(int32_t);
+}
+
 // Lengths (and with `more` the rows added to them) inside [0, L_cap].
 int q8_lens_check(const int32_t* seq_lens, const int32_t* more, int fixed, int most, int B, int L_cap,
                   hipStream_t stream) {
@@ -678,9 +684,12 @@ int glide_q8_commit(const glide_q8_cache* caches, int layers, const int32_t* seq
                     const int32_t* accept_len, const int32_t* path, int32_t* seq_lens_out, int B,
                     int N, int H_kv, int D, int L_cap, int kind, hipStream_t stream) {
   glide::Q8CommitArgs a{};
-  if (!caches || !seq_lens || !accept_len || !seq_lens_out || seq_lens_out == seq_lens) return GLIDE_EINVAL;
+  if (!caches || !seq_lens || !accept_len || !seq_lens_out) return GLIDE_EINVAL;
   if (layers < 1 || layers > glide::kQ8MaxLayers || N < 1 || N > glide::kMaxNodes) return GLIDE_EINVAL;
   if (!q8_sizes_ok(B, H_kv, D, L_cap, kind)) return GLIDE_EINVAL;
+  // the new lengths are written while other workgroups still read these
+  if (overlap(seq_lens_out, B, seq_lens, B) || overlap(seq_lens_out, B, accept_len, B)) return GLIDE_EINVAL;
+  if (path && overlap(seq_lens_out, B, path, (size_t)B * N)) return GLIDE_EINVAL;
   const void* tails[glide::kQ8MaxLayers];
   bool sorted = true;
   for (int l = 0; l < layers; ++l) {

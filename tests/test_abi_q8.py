@@ -212,3 +212,13 @@ def test_binding_rejects_host_tensors():
 def test_rope_rejects_heads_whose_pieces_pass_an_int(lib, dtype, H, Hkv):
     """A row is 8 or 16 pieces for the threads of its token, counted in 32 bits."""
     assert _rope(lib, H=H, Hkv=Hkv, B=1, T=1, dtype=dtype) == EINVAL
+
+
+@pytest.mark.parametrize("bad", [dict(acc=FAKE + 64), dict(path=FAKE + 64), dict(lens=FAKE + 68), dict(lens=FAKE + 60),
+                                 dict(acc=FAKE + 68), dict(acc=FAKE + 60), dict(path=FAKE + 68),
+                                 dict(path=FAKE + 64 - 4 * 32 + 4), dict(path=FAKE)])
+def test_commit_rejects_lengths_out_that_overlap_what_is_read(lib, bad):
+    """Workgroups read lengths, counts and paths while one of them writes the new
+    lengths: of two sequences and 16 nodes here."""
+    apart = dict(lens=FAKE + 1024, acc=FAKE + 2048, path=FAKE + 4096, out=FAKE + 64, B=2)
+    assert _commit(lib, **{**apart, **bad}) == EINVAL
