@@ -75,6 +75,13 @@ __device__ __forceinline__ int depth_of(const int32_t* parents, int t) {
   }
 }
 
+// What a wave's lanes wrote to LDS before is there for its other lanes behind this.
+__device__ __forceinline__ void wave_meets() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 // Two pieces of one row.  LAYOUT
 //   0: pairs (2i, 2i + 1): piece j of either half of the row;
 //   1: pairs (i, i + rot / 2) where the pieces of a pair's two dims are whole
@@ -121,13 +128,13 @@ struct Item {
     } else {
 #pragma unroll
       for (int e = 0; e < V; ++e) row[d1 + e] = x1[e], row[d2 + e] = x2[e];
-      __builtin_amdgcn_wave_barrier();  // a row is one wave's
+      wave_meets();  // a row is one wave's
 #pragma unroll
       for (int e = 0; e < V; ++e) {
         x1[e] = turned(x1[e], d1 + e, cs, rot, half, row);
         x2[e] = turned(x2[e], d2 + e, cs, rot, half, row);
       }
-      __builtin_amdgcn_wave_barrier();
+      wave_meets();
     }
     store_piece(out + d1, x1);
     store_piece(out + d2, x2);

@@ -187,3 +187,27 @@ def test_refusals():
         with pytest.raises((ValueError, glide.GlideError)):
             glide.glide_rope(*args, **kw)
     glide.glide_rope(k.expand(2, 4, 3, 128), None, freqs, q, None)  # rows that are read may share memory
+
+
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("rot", [50, 126, 12])
+def test_pairs_across_pieces_over_many_heads(dtype, rot):
+    """Pairs whose dims lie in different pieces, more heads than a workgroup's
+    threads take at once, so that a row's copy in LDS is replaced several times;
+    into other rows and in place."""
+    require_gpu()
+    B, T, H, Hk = 2, 3, 96, 37
+    freqs, m = glide.rope_frequencies(rot)
+    q, k = cpu_normal((B, T, H, 128), 8, dtype).cuda(), cpu_normal((B, T, Hk, 128), 9, dtype).cuda()
+    pos = np.array([[0, 7, 100001], [5, 6, 4000]], dtype=np.int32)
+    where = torch.from_numpy(pos).cuda()
+    for back in (False, True):
+        say("many heads", str(dtype), rot, back)
+        qo, ko = torch.empty_like(q), torch.empty_like(k)
+        glide.glide_rope(q, k, freqs, qo, ko, positions=where, backward=back)
+        qi, ki = q.clone(), k.clone()
+        glide.glide_rope(qi, ki, freqs, qi, ki, positions=where, backward=back)
+        torch.cuda.synchronize()
+        for got, x in ((qo, q), (ko, k)):
+            _check(got, x, pos, f64(freqs), m, False, back)
+        assert torch.equal(qi, qo) and torch.equal(ki, ko)
