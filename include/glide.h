@@ -467,7 +467,10 @@ int glide_rope(const glide_rope_rows* q, const glide_rope_rows* k, const double*
 #define GLIDE_ROPE_YARN   3  /* frequencies that turn less than once over original_len
                                 positions divided by factor, those that turn 32
                                 times or more kept, a linear ramp of the number of
-                                turns between; m = 0.1 ln(factor) + 1 */
+                                turns between; m = 0.1 ln(factor) + 1.  (Some
+                                published models ramp over the pairs' index
+                                between two rounded ends instead: freqs for such
+                                a model are the caller's own.) */
 
 /*
  * glide_rope_frequencies -- the frequencies and the factor m of a rotary
@@ -559,7 +562,8 @@ int glide_q8_read(const glide_q8_cache* cache, const int32_t* seq_lens, void* k_
  *   which workgroup runs when.
  * Precision: scores, sums and outputs accumulate in float32 from exact codes;
  * probabilities enter the PV product with 11 significant bits (those below
- * 2^-21 of a row's largest with fewer).  Tree rows that are not finite reach
+ * 2^-21 of a row's largest with fewer; where a block's values are below about
+ * 2^-110, those below up to 2^-14 of it).  Tree rows that are not finite reach
  * only the nodes that see them.
  */
 size_t glide_q8_tree_attn_workspace(int B, int N, int H, int H_kv, int D, int L_cap, int max_splits);

@@ -922,7 +922,8 @@ def glide_q8_commit(caches, seq_lens, accept_len, path, seq_lens_out, nodes=None
     """Commits the accepted rows of a verification step in every layer's 8-bit
     cache and writes the new lengths.  caches: a Q8Cache per layer; path [B, N]
     as glide_verify_commit gives it, or None for a chain (of at most `nodes`
-    rows, by default 64).  See include/glide.h."""
+    rows, by default 64).  seq_lens_out shares no memory with the other tensors.
+    See include/glide.h."""
     if nodes is None:
         nodes = path.shape[1] if isinstance(path, torch.Tensor) and path.dim() == 2 else MAX_NODES
     status = (_native or _bind()).q8_commit(caches, seq_lens, accept_len, path, seq_lens_out, nodes, stream)

@@ -31,6 +31,7 @@
 //    It moves up only when one passes 2^15 (like the running maximum, c moves
 //    rarely), so a product keeps 11 bits down to 2^-21 of the largest.  With
 //    bfloat16 the rounding of P alone is as far off as that of the output.
+//    c ends at 2^126; where it would pass that, the accumulators fall instead.
 // Ring rows are bfloat16: their products take bfloat16 operands, P as the sum
 // of two.  Sums, maxima and outputs are float32.
 //
@@ -46,7 +47,9 @@
 // what is rare stands apart, and little is unrolled outside the loop over blocks.
 // Several groups of rows are bound by the conversions, the softmax and the matrix
 // instructions in turn (eight sequences of 52 heads, 64 tree rows, 677 MB: 145 us,
-// 4.7 TB/s).
+// 4.7 TB/s; the vector units busy half of it, the matrix cores a quarter).
+// Many short pairs pay what lies around the stream once for every 256 of them (32
+// sequences of 52 heads, one row, 100 tokens, 46 MB: 46 us).
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>

@@ -16,7 +16,8 @@
 // rows are on their way, then every thread turns two 16-byte pieces of a row at a
 // time, which lie side by side across its lanes (two pieces of a lane side by side
 // instead: 37 us).  Bound: the memory's copy rate (four 2048-token sequences of 40
-// heads, 168 MB in 33 us, 5.1 TB/s); a decoding step's few rows take a launch.
+// heads, 168 MB in 33 us, 5.1 TB/s); a decoding step's few rows take a launch,
+// and a tree's one load more an ancestor.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -63,8 +64,9 @@ __device__ __forceinline__ void store_piece(float* p, const float (&x)[4]) {
   *(float4*)p = make_float4(x[0], x[1], x[2], x[3]);
 }
 
-// Depth of node t: its ancestors, followed up by one lane (a chain of at most
-// 63 parents; those outside [-1, node) count as -1).
+// Depth of node t: its ancestors, one load behind the other, followed up by every
+// lane with an angle (at most 63; parents outside [-1, node) count as -1).  Nodes
+// in one chain behind 512 tokens, 32 heads: five 3.3 us, 64 8.6; 64 roots 3.2.
 __device__ __forceinline__ int depth_of(const int32_t* parents, int t) {
   int d = 0, n = t;
   while (true) {
